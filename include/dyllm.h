@@ -102,6 +102,23 @@ typedef struct {
                  attention row; written by the dense step and for the exact rows of every sparse step */
 } dyllm_layer_cache;
 
+/* The key/value cache in 8 bits: for every (token, key-value head) a vector of head_dim codes and one fp32
+ * scale, value = code * scale.  [Sec. 5: the caches are the method's memory cost]
+ *   DYLLM_E4M3  codes are OCP e4m3; the scale is 2^max(e, -100) with the smallest e for which the largest
+ *               magnitude of the vector is at most 448 * 2^e.  Kernels read the exponent of such a scale
+ *               alone: it has to be a power of two (or NaN).
+ *   DYLLM_INT8  with m = max(largest magnitude, 2^-100): scale = m / 127, code = rint(x * (127 / m)).
+ * A vector that holds an infinity or NaN is stored with a NaN for its scale and reads back as NaN. */
+#define DYLLM_E4M3 0
+#define DYLLM_INT8 1
+typedef struct {
+  void *k;         /* [B, L, Hkv, dh] codes of the keys, which are stored AFTER the rotary embedding */
+  void *v;         /* [B, L, Hkv, dh] codes of the values */
+  float *k_scale;  /* [B, Hkv, L] */
+  float *v_scale;  /* [B, Hkv, L] */
+  int32_t format;  /* DYLLM_E4M3 or DYLLM_INT8 */
+} dyllm_quant_cache;
+
 /* A set of tokens: ascending, unique token ids, grouped by sequence. */
 typedef struct {
   int32_t *idx;     /* [cap] token ids b*L+i; entries beyond the count are undefined; may be NULL
@@ -315,6 +332,66 @@ int dyllm_stack_step(dyllm_ctx *ctx, int32_t n_layers, const dyllm_layer_weights
 int dyllm_stack_full_step(dyllm_ctx *ctx, int32_t n_layers, const dyllm_layer_weights *w,
                           dyllm_layer_cache *caches, const void *x, int32_t B, int32_t L,
                           void *stream);
+
+/* ---- layers with normalised query and key heads; a key/value cache in 8 bits ------------------------
+ * For the entry points of this section, besides the conventions above: rows == NULL means all B*L
+ * tokens (row j = token j); tensors that start at no multiple of 16 bytes are refused (INVALID_ARG), scales
+ * and lengths need their element's alignment only; outputs must not overlap inputs; list entries must be
+ * token ids in [0, B*L), each of them once (not looked at). */
+
+/* RMSNorm of every query and key head, rotary embedding, and the merge of keys and values, in one pass over
+ * raw projections.  [Alg. 3: q_proj, k_proj / v_proj merge lines, of layers that normalise q and k]
+ * Row j of qkv: the query heads, key heads and value heads of token r = rows->idx[j] as the projections left them,
+ * [(H + 2*Hkv) * dh] elements, ld elements from one row to the next (ld >= that; a multiple of 8,
+ * fp32: of 4).  For every head vector x of q with gain g_q, of k with gain g_k:
+ *   n = x / sqrt(mean(x^2) + rms_eps) * g   (gain NULL: n = x),
+ *   y = n rotated by the rotary embedding at position r mod L;
+ * q_out[j] = y of q, layout [count, H, dh]; cache->k[r] = y of k, cache->v[r] = the value heads as they are.  Other
+ * rows of the caches stay; cache->c and cache->out are not looked at.  g_q, g_k: [dh] or NULL. */
+int dyllm_head_norm_rope(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
+                         const dyllm_index_list *rows, int32_t B, int32_t L, dyllm_layer_cache *cache,
+                         void *q_out, void *stream);
+
+/* The same with keys and values quantised as they are written: codes and scales of the rows' tokens, of the
+ * values before any rounding to the storage type. */
+int dyllm_head_norm_rope_quant(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
+                               const dyllm_index_list *rows, int32_t B, int32_t L, dyllm_quant_cache *cache,
+                               void *q_out, void *stream);
+
+/* Quantises finished key and value rows into the cache: k, v are [count, Hkv, dh], row j belongs to token
+ * rows->idx[j].  With rows == NULL it converts a whole cache of the storage type. */
+int dyllm_quant_write(dyllm_ctx *ctx, const void *k, const void *v, const dyllm_index_list *rows, int32_t B,
+                      int32_t L, dyllm_quant_cache *cache, void *stream);
+
+/* Reads rows of the cache back: k_out[j], v_out[j] = code * scale of token rows->idx[j], rounded to the
+ * storage type, [count, Hkv, dh]. */
+int dyllm_quant_read(dyllm_ctx *ctx, const dyllm_quant_cache *cache, const dyllm_index_list *rows, int32_t B,
+                     int32_t L, void *k_out, void *v_out, void *stream);
+
+/* dyllm_partial_attention over the cache in 8 bits.  [Sec. 3.3 salient path; Alg. 3: C_sal]
+ * kv_len: NULL, or [B] device int32: sequence b has the keys at positions [0, kv_len[b]) (clamped to [0, L]);
+ * what lies behind them, padding, is never used.  The rows of a sequence without keys are zero.
+ * q_sal: [count, H, dh]; c_sal_out: [count, H*dh]. */
+int dyllm_partial_attention_quant(dyllm_ctx *ctx, const void *q_sal, const dyllm_quant_cache *cache,
+                                  const int32_t *kv_len, const dyllm_index_list *rows, int32_t B, int32_t L,
+                                  void *c_sal_out, void *stream);
+
+/* dyllm_qkv_refresh of such a layer: RMSNorm of the rows of x, projections (+ biases), then the pass of
+ * dyllm_head_norm_rope over the projections in fp32.  Keys and values go to `cache` or to `quant`: exactly
+ * one of them is given, the other is NULL.  rows == NULL needs a context with max_rows covering B*L. */
+int dyllm_qkv_refresh_normed(dyllm_ctx *ctx, const dyllm_layer_weights *w, const void *g_q, const void *g_k,
+                             const void *x, const dyllm_index_list *rows, int32_t B, int32_t L,
+                             dyllm_layer_cache *cache, dyllm_quant_cache *quant, void *q_sal_out, void *stream);
+
+/* One layer of SparseStep over a cache in 8 bits.  [Alg. 3 layer body]
+ * = dyllm_qkv_refresh_normed(idx_in, quant) -> dyllm_partial_attention_quant -> dyllm_saliency(commit) ->
+ *   dyllm_compact -> dyllm_salient_ffn(idx_out); arguments as in dyllm_layer_step.  Of `cache` only c and out are
+ * used (k, v and lse may be NULL).  g_q, g_k: NULL for layers without such norms.  A dense step is one whose list
+ * holds all tokens, with tau > 1. */
+int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const void *g_q, const void *g_k,
+                           dyllm_layer_cache *cache, dyllm_quant_cache *quant, const int32_t *kv_len, const void *x,
+                           const dyllm_index_list *idx_in, int32_t B, int32_t L, float tau,
+                           dyllm_index_list *idx_out, float *cos_out, void *stream);
 
 /* Per-stage timing of dyllm_layer_step / dyllm_full_step for measurement.  After
  * dyllm_profile_begin the next max_calls (<= 4096) step calls on this context record a HIP event on

@@ -26,6 +26,8 @@ SYMBOLS = [
     "dyllm_partial_attention", "dyllm_salient_ffn", "dyllm_layer_step", "dyllm_layer_step_approx",
     "dyllm_stack_step_approx", "dyllm_merge_lists", "dyllm_step_kind", "dyllm_denoise_step", "dyllm_full_step",
     "dyllm_stack_step", "dyllm_stack_full_step", "dyllm_pack_weight",
+    "dyllm_head_norm_rope", "dyllm_head_norm_rope_quant", "dyllm_quant_write", "dyllm_quant_read",
+    "dyllm_partial_attention_quant", "dyllm_qkv_refresh_normed", "dyllm_layer_step_quant",
     "dyllm_profile_begin", "dyllm_profile_end", "dyllm_stage_count", "dyllm_stage_name",
 ]
 
@@ -56,6 +58,11 @@ class LayerCache(C.Structure):
 
 class IndexListC(C.Structure):
     _fields_ = [("idx", C.c_void_p), ("offsets", C.c_void_p), ("cap", C.c_int32)]
+
+
+class QuantCacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("format", C.c_int32)]
 
 
 class Schedule(C.Structure):
@@ -108,6 +115,15 @@ def load_library() -> C.CDLL:
     lib.dyllm_stack_step.argtypes = [vp, i32, P(LayerWeights), P(LayerCache), vp, P(IndexListC), i32, i32, f32,
                                      P(IndexListC), vp, vp]
     lib.dyllm_stack_full_step.argtypes = [vp, i32, P(LayerWeights), P(LayerCache), vp, i32, i32, vp]
+    P_idx, P_q, i64 = P(IndexListC), P(QuantCacheC), C.c_int64
+    lib.dyllm_head_norm_rope.argtypes = [vp, vp, i64, vp, vp, P_idx, i32, i32, P(LayerCache), vp, vp]
+    lib.dyllm_head_norm_rope_quant.argtypes = [vp, vp, i64, vp, vp, P_idx, i32, i32, P_q, vp, vp]
+    lib.dyllm_quant_write.argtypes = [vp, vp, vp, P_idx, i32, i32, P_q, vp]
+    lib.dyllm_quant_read.argtypes = [vp, P_q, P_idx, i32, i32, vp, vp, vp]
+    lib.dyllm_partial_attention_quant.argtypes = [vp, vp, P_q, vp, P_idx, i32, i32, vp, vp]
+    lib.dyllm_qkv_refresh_normed.argtypes = [vp, P(LayerWeights), vp, vp, vp, P_idx, i32, i32, P(LayerCache), P_q, vp, vp]
+    lib.dyllm_layer_step_quant.argtypes = [vp, P(LayerWeights), vp, vp, P(LayerCache), P_q, vp, vp, P_idx, i32, i32, f32,
+                                           P_idx, vp, vp]
     lib.dyllm_profile_begin.argtypes = [vp, i32]
     lib.dyllm_profile_end.argtypes = [vp, P(f32), P(i32)]
     lib.dyllm_stage_count.argtypes = []
@@ -153,6 +169,33 @@ class IndexList:
                          torch.zeros(B + 1, dtype=torch.int32, device=device))
 
 
+E4M3, INT8 = 0, 1
+CODES = {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
+
+
+class QuantCache:
+    """Key/value cache in 8 bits: codes k, v [B, L, Hkv, dh] (torch.float8_e4m3fn or torch.int8), scales [B, Hkv, L] fp32."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        if k.dtype not in CODES or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("codes are two [B, L, Hkv, dh] tensors of float8_e4m3fn or int8")
+        B, L, Hkv, _ = k.shape
+        for s in (k_scale, v_scale):
+            if s.dtype != torch.float32 or tuple(s.shape) != (B, Hkv, L):
+                raise ValueError("scales are fp32 [B, Hkv, L] tensors")
+        for t in (v, k_scale, v_scale):
+            if t.device != k.device:
+                raise ValueError("the cache's tensors are on different devices")
+        self.k, self.v, self.k_scale, self.v_scale, self.format = k, v, k_scale, v_scale, CODES[k.dtype]
+        self.c = QuantCacheC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.format)
+
+    @staticmethod
+    def empty(B: int, L: int, Hkv: int, dh: int, codes=torch.float8_e4m3fn, device="cuda") -> "QuantCache":
+        """A cache of zeros."""
+        c = [torch.zeros(B, L, Hkv, dh, dtype=torch.int8, device=device).view(codes) for _ in range(2)]
+        return QuantCache(*c, *(torch.zeros(B, Hkv, L, dtype=torch.float32, device=device) for _ in range(2)))
+
+
 def make_weights(tensors: dict) -> LayerWeights:
     w = LayerWeights()
     for name, _ in LayerWeights._fields_:
@@ -162,9 +205,8 @@ def make_weights(tensors: dict) -> LayerWeights:
 
 
 def make_cache(k, v, c, out, lse=None) -> LayerCache:
-    """lse: fp32 [B, L, H] tensor for the log-normaliser cache, or None."""
-    return LayerCache(k.data_ptr(), v.data_ptr(), c.data_ptr(), out.data_ptr(),
-                      lse.data_ptr() if lse is not None else None)
+    """lse: fp32 [B, L, H] tensor for the log-normaliser cache, or None.  k, v: None where they are held in 8 bits."""
+    return LayerCache(*(None if t is None else t.data_ptr() for t in (k, v, c, out, lse)))
 
 
 def pack_weight(src: torch.Tensor, dst: torch.Tensor) -> None:
@@ -313,6 +355,101 @@ class Context:
                                                 C.byref(cc) if cc is not None else None, B, L, C.byref(kc), oa,
                                                 _stream()))
         return int(self.lib.dyllm_step_kind(C.byref(sched), t))
+
+    # ---- normalised query and key heads; the cache in 8 bits.  Tensors are checked against the context: type, number of elements, device.
+
+    def _arg(self, t, numel, what, dtype=None):
+        dtype = dtype or (torch.float32 if self.cfg.dtype == F32 else torch.bfloat16)
+        if t.dtype != dtype or t.numel() < numel or not t.is_contiguous():
+            raise ValueError("%s: a contiguous %s tensor of at least %d elements is wanted" % (what, dtype, numel))
+        if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+            raise ValueError("%s: not on the current device" % what)
+        return t.data_ptr()
+
+    def _gain(self, g, what):
+        return None if g is None else self._arg(g, self.cfg.head_dim, what)
+
+    def _rows(self, rows, B, L):
+        """(the list's structure or None, rows at most)"""
+        if rows is None:
+            return None, B * L
+        if rows.offsets.numel() < B + 1:
+            raise ValueError("rows: %d offsets are wanted" % (B + 1))
+        return C.byref(rows.c()), rows.cap
+
+    def _quant(self, cache: QuantCache, B, L):
+        b, l, hkv, dh = cache.k.shape
+        if (hkv, dh) != (self.cfg.n_kv_heads, self.cfg.head_dim) or (b, l) != (B, L):
+            raise ValueError("the 8-bit cache is [%d, %d, %d, %d], the call's [%d, %d, %d, %d]"
+                             % (b, l, hkv, dh, B, L, self.cfg.n_kv_heads, self.cfg.head_dim))
+        if cache.k.device.index != torch.cuda.current_device():
+            raise ValueError("the 8-bit cache is not on the current device")
+        return C.byref(cache.c)
+
+    def _qkv(self, qkv, n):
+        """(pointer, row stride) of raw projections [n, (H + 2 Hkv) dh], whose rows may lie further apart than they are long"""
+        width = (self.cfg.n_heads + 2 * self.cfg.n_kv_heads) * self.cfg.head_dim
+        if qkv.dim() != 2 or qkv.shape[1] != width or qkv.shape[0] < n or qkv.stride(1) != 1 or (n > 1 and qkv.stride(0) < width):
+            raise ValueError("qkv: [%d, %d] with neighbouring columns is wanted" % (n, width))
+        ld = qkv.stride(0) if qkv.shape[0] > 1 else width
+        if qkv.dtype != (torch.float32 if self.cfg.dtype == F32 else torch.bfloat16) or qkv.device.index != torch.cuda.current_device():
+            raise ValueError("qkv: of another type or device than the context's")
+        return qkv.data_ptr(), ld
+
+    def head_norm_rope(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: LayerCache, q_out):
+        """qkv: [n, (H + 2 Hkv) dh], rows may be strided; g_q, g_k: [dh] or None; rows None: all B*L tokens."""
+        r, n = self._rows(rows, B, L)
+        p, ld = self._qkv(qkv, n)
+        q = self._arg(q_out, n * self.cfg.n_heads * self.cfg.head_dim, "q_out")
+        self._check(self.lib.dyllm_head_norm_rope(self.h, p, ld, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), r, B, L,
+                                                  C.byref(cache), q, _stream()))
+
+    def head_norm_rope_quant(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: QuantCache, q_out):
+        r, n = self._rows(rows, B, L)
+        p, ld = self._qkv(qkv, n)
+        q = self._arg(q_out, n * self.cfg.n_heads * self.cfg.head_dim, "q_out")
+        self._check(self.lib.dyllm_head_norm_rope_quant(self.h, p, ld, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), r, B,
+                                                        L, self._quant(cache, B, L), q, _stream()))
+
+    def quant_write(self, k, v, rows: Optional[IndexList], B, L, cache: QuantCache):
+        r, n = self._rows(rows, B, L)
+        n *= self.cfg.n_kv_heads * self.cfg.head_dim
+        self._check(self.lib.dyllm_quant_write(self.h, self._arg(k, n, "k"), self._arg(v, n, "v"), r, B, L,
+                                               self._quant(cache, B, L), _stream()))
+
+    def quant_read(self, cache: QuantCache, rows: Optional[IndexList], B, L, k_out, v_out):
+        r, n = self._rows(rows, B, L)
+        n *= self.cfg.n_kv_heads * self.cfg.head_dim
+        self._check(self.lib.dyllm_quant_read(self.h, self._quant(cache, B, L), r, B, L, self._arg(k_out, n, "k_out"),
+                                              self._arg(v_out, n, "v_out"), _stream()))
+
+    def partial_attention_quant(self, q_sal, cache: QuantCache, rows: Optional[IndexList], B, L, c_sal_out, kv_len=None):
+        """kv_len: int32 [B] device tensor (keys of each sequence) or None."""
+        r, n = self._rows(rows, B, L)
+        n *= self.cfg.n_heads * self.cfg.head_dim
+        self._check(self.lib.dyllm_partial_attention_quant(
+            self.h, self._arg(q_sal, n, "q_sal"), self._quant(cache, B, L),
+            None if kv_len is None else self._arg(kv_len, B, "kv_len", torch.int32), r, B, L,
+            self._arg(c_sal_out, n, "c_sal_out"), _stream()))
+
+    def qkv_refresh_normed(self, w: LayerWeights, g_q, g_k, x, rows: Optional[IndexList], B, L, cache, q_sal_out):
+        """cache: LayerCache (storage type) or QuantCache."""
+        r, n = self._rows(rows, B, L)
+        quant = isinstance(cache, QuantCache)
+        self._check(self.lib.dyllm_qkv_refresh_normed(
+            self.h, C.byref(w), self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), self._arg(x, B * L * self.cfg.hidden, "x"), r,
+            B, L, None if quant else C.byref(cache), self._quant(cache, B, L) if quant else None,
+            self._arg(q_sal_out, n * self.cfg.n_heads * self.cfg.head_dim, "q_sal_out"), _stream()))
+
+    def layer_step_quant(self, w: LayerWeights, g_q, g_k, cache: LayerCache, quant: QuantCache, x, idx_in: IndexList, B, L,
+                         tau, idx_out: IndexList, cos_out=None, kv_len=None):
+        """Of cache only c and out are used."""
+        i, o = self._rows(idx_in, B, L)[0], idx_out.c()
+        self._check(self.lib.dyllm_layer_step_quant(
+            self.h, C.byref(w), self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), C.byref(cache), self._quant(quant, B, L),
+            None if kv_len is None else self._arg(kv_len, B, "kv_len", torch.int32),
+            self._arg(x, B * L * self.cfg.hidden, "x"), i, B, L, tau, C.byref(o),
+            None if cos_out is None else self._arg(cos_out, idx_in.cap, "cos_out", torch.float32), _stream()))
 
     def full_step(self, w: LayerWeights, cache: LayerCache, x, B, L):
         self._check(self.lib.dyllm_full_step(self.h, C.byref(w), C.byref(cache), _ptr(x), B, L, _stream()))

@@ -27,6 +27,7 @@ struct dyllm_ctx {
   float *part_o;   // fp32 scratch shared by consecutive stages: raw GEMM results / attention partials
   float *part_ml;
   size_t part_elems;
+  size_t quant_part_elems;  // ... as many of these as attention over the 8-bit cache may use (few rows of long sequences: more splits)
   void *dv_full;   // [R, dkv] value residuals of the approximate path, by token or by sequence; all zero between calls
   void *dc;        // [R, dq] approximate context residual of every token
   void *csal;      // [R, dq] exact context rows of the salient tokens (approximate path)
@@ -55,7 +56,7 @@ namespace {
 
 struct Layout {
   size_t ns, qs, part_o, part_ml, cosb, flag, hs, fs, act, status, rope, dv_full, dc, csal, pos, win_idx, win_off, ksal, scan, total;
-  size_t part_elems;
+  size_t part_elems, quant_part_elems;
 };
 
 // the status word, a counter, and from PLANS_AT on the plans
@@ -78,8 +79,11 @@ Layout make_layout(const dyllm_layer_cfg &c) {
   const size_t prow = R < 2048 ? R : 2048;
   const size_t widest = dq + 2 * dkv > d ? dq + 2 * dkv : d;
   l.part_elems = 16 * prow * dq > R * widest ? 16 * prow * dq : R * widest;
-  l.part_o = take(l.part_elems * 4);
-  l.part_ml = take(l.part_elems / c.head_dim * 2 * 4);
+  // (attention over the 8-bit cache: up to 128 splits of 32 rows)
+  const size_t few = 128 * (R < 32 ? R : 32) * dq;
+  l.quant_part_elems = l.part_elems > few ? l.part_elems : few;
+  l.part_o = take(l.quant_part_elems * 4);
+  l.part_ml = take(l.quant_part_elems / c.head_dim * 2 * 4);
   l.cosb = take(R * 4);
   l.flag = take(R);
   l.hs = take(R * d * 4);
@@ -522,6 +526,109 @@ int enqueue_dense_layer(dyllm_ctx *ctx, const dyllm_layer_weights *w, dyllm_laye
   return rc;
 }
 
+// ---- layers with normalised query and key heads, caches in 8 bits ----------------------------------
+
+bool misaligned(const void *p) { return (uintptr_t)p & 15; }
+
+int check_quant(dyllm_ctx *ctx, const dyllm_quant_cache *q) {
+  if (!q || !q->k || !q->v || !q->k_scale || !q->v_scale) return fail(ctx, DYLLM_ERR_INVALID_ARG, "8-bit cache pointer is NULL");
+  if (q->format != DYLLM_E4M3 && q->format != DYLLM_INT8) return fail(ctx, DYLLM_ERR_INVALID_ARG, "unknown format of the 8-bit cache");
+  if (misaligned(q->k) || misaligned(q->v) || ((uintptr_t)q->k_scale & 3) || ((uintptr_t)q->v_scale & 3))
+    return fail(ctx, DYLLM_ERR_INVALID_ARG, "8-bit cache is misaligned");
+  return DYLLM_OK;
+}
+
+QuantCache quant_of(const dyllm_quant_cache *q) {
+  return QuantCache{(uint8_t *)q->k, (uint8_t *)q->v, q->k_scale, q->v_scale};
+}
+
+// a list, or all tokens (rows == NULL); scratch: the call keeps something of every row in the workspace
+int check_rows(dyllm_ctx *ctx, const dyllm_index_list *rows, int B, int L, bool scratch, Rows *r) {
+  int rc;
+  if ((rc = check_bl(ctx, B, L))) return rc;
+  if (rows) {
+    if ((rc = check_list(ctx, rows, "rows"))) return rc;
+    *r = rows_of(rows, B);
+    return DYLLM_OK;
+  }
+  if (scratch && (long)B * L > ctx->rows_cap) return fail(ctx, DYLLM_ERR_CAPACITY, "B*L exceeds the context's max_rows");
+  *r = Rows{nullptr, nullptr, B * L};
+  return DYLLM_OK;
+}
+
+int check_gains(dyllm_ctx *ctx, const void *g_q, const void *g_k) {
+  if (misaligned(g_q) || misaligned(g_k)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "g_q / g_k is misaligned");
+  return DYLLM_OK;
+}
+
+HeadsArgs heads_args(const dyllm_ctx *ctx, const void *g_q, const void *g_k, Rows rows, int L, void *q_out) {
+  const dyllm_layer_cfg &c = ctx->cfg;
+  HeadsArgs a;
+  a.g_q = g_q; a.g_k = g_k; a.eps = c.rms_eps; a.tab = ctx->rope;
+  a.rows = rows; a.L = L; a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.q_out = q_out;
+  return a;
+}
+int heads_to(HeadsArgs *a, const dyllm_layer_cache *cache, const dyllm_quant_cache *quant) {
+  if (quant) {
+    a->quant = quant_of(quant);
+    return 1 + quant->format;
+  }
+  a->kc = cache->k; a->vc = cache->v;
+  return 0;
+}
+
+int head_norm_rope(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k, const dyllm_index_list *rows,
+                   int B, int L, const dyllm_layer_cache *cache, const dyllm_quant_cache *quant, void *q_out, hipStream_t s) {
+  int rc;
+  Rows r;
+  if (!qkv || !q_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(qkv) || misaligned(q_out)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_gains(ctx, g_q, g_k))) return rc;
+  if ((rc = check_rows(ctx, rows, B, L, false, &r))) return rc;
+  if (ld < ctx->dq + 2 * ctx->dkv || ld * (int64_t)ctx->esz % 16) return fail(ctx, DYLLM_ERR_BAD_SHAPE, "ld is too small or no multiple of 16 bytes");
+  HeadsArgs a = heads_args(ctx, g_q, g_k, r, L, q_out);
+  a.q = qkv;
+  a.k = (const char *)qkv + (size_t)ctx->dq * ctx->esz;
+  a.v = (const char *)qkv + (size_t)(ctx->dq + ctx->dkv) * ctx->esz;
+  a.ld = (size_t)ld;
+  const int to = heads_to(&a, cache, quant);
+  launch_heads(dt(ctx), a, false, ctx->cfg.head_dim, to, s);
+  return check_launch(ctx, "head norm");
+}
+
+// norm, projections, then norm and rotation of the heads on the GEMM's fp32 sums
+int enqueue_qkv_normed(dyllm_ctx *ctx, const dyllm_layer_weights *w, const void *g_q, const void *g_k, const void *x, Rows rows, int B,
+                       int L, const dyllm_layer_cache *cache, const dyllm_quant_cache *quant, void *q_out, hipStream_t s) {
+  const dyllm_layer_cfg &c = ctx->cfg;
+  WSeg seg;
+  seg.w[0] = w->wq; seg.w[1] = w->wk; seg.w[2] = w->wv;
+  seg.n_end[0] = ctx->dq; seg.n_end[1] = ctx->dq + ctx->dkv; seg.n_end[2] = ctx->dq + 2 * ctx->dkv;
+  const GemmA A{ctx->ns, nullptr, c.hidden};
+  const QkvOut beside = raw_beside(c.n_heads, c.n_kv_heads, c.head_dim, (size_t)B * L);
+  const PlanJob job = plan_gemm_raw(dt(ctx), A, rows, c.hidden, seg, ctx->part_elems, ctx->plan, beside);
+  launch_gather_rmsnorm(dt(ctx), x, w->g_attn, rows, c.hidden, c.rms_eps, ctx->ns, 0, job.make, s);
+  HeadsArgs a = heads_args(ctx, g_q, g_k, rows, L, q_out);
+  a.splits = launch_gemm_raw(dt(ctx), A, rows, c.hidden, seg, ctx->part_o, ctx->part_elems, ctx->plan, job, beside, s);
+  a.q = ctx->part_o; a.k = ctx->part_o + ctx->dq; a.v = ctx->part_o + ctx->dq + ctx->dkv;
+  a.ld = (size_t)(ctx->dq + 2 * ctx->dkv);
+  a.bq = w->bq; a.bk = w->bk; a.bv = w->bv;
+  const int to = heads_to(&a, cache, quant);
+  launch_heads(dt(ctx), a, true, c.head_dim, to, s);
+  return check_launch(ctx, "qkv refresh, normalised heads");
+}
+
+int enqueue_attention_quant(dyllm_ctx *ctx, const void *q, const dyllm_quant_cache *quant, const int32_t *kv_len, Rows rows,
+                            const int32_t *offsets, int B, int L, void *out, hipStream_t s) {
+  const dyllm_layer_cfg &c = ctx->cfg;
+  AttnArgs a{};
+  a.q = q; a.rows = rows; a.offsets = offsets;
+  a.B = B; a.L = L; a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.dh = c.head_dim;
+  a.part_o = ctx->part_o; a.part_ml = ctx->part_ml; a.out = out;
+  attention_quant_plan(dt(ctx), ctx->quant_part_elems, &a);
+  launch_attention_quant(dt(ctx), a, QuantAttn{quant_of(quant), kv_len, quant->format}, s);
+  return check_launch(ctx, "attention over the 8-bit cache");
+}
+
 }  // namespace
 
 extern "C" {
@@ -573,6 +680,7 @@ int dyllm_create(const dyllm_layer_cfg *cfg, dyllm_ctx **out) {
   ctx->ns = b + l.ns; ctx->qs = b + l.qs;
   ctx->part_o = (float *)(b + l.part_o); ctx->part_ml = (float *)(b + l.part_ml);
   ctx->part_elems = l.part_elems;
+  ctx->quant_part_elems = l.quant_part_elems;
   ctx->cosb = (float *)(b + l.cosb); ctx->flag = (uint8_t *)(b + l.flag);
   ctx->hs = (float *)(b + l.hs); ctx->fs = b + l.fs; ctx->act = b + l.act;
   ctx->status = (int32_t *)(b + l.status); ctx->rope = (float *)(b + l.rope);
@@ -945,6 +1053,115 @@ int dyllm_stack_full_step(dyllm_ctx *ctx, int32_t n_layers, const dyllm_layer_we
                                   (hipStream_t)stream)))
       return rc;
   return DYLLM_OK;
+}
+
+int dyllm_head_norm_rope(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
+                         const dyllm_index_list *rows, int32_t B, int32_t L, dyllm_layer_cache *cache,
+                         void *q_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  if (!cache || !cache->k || !cache->v) return fail(ctx, DYLLM_ERR_INVALID_ARG, "cache pointer is NULL");
+  if (misaligned(cache->k) || misaligned(cache->v)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  return head_norm_rope(ctx, qkv, ld, g_q, g_k, rows, B, L, cache, nullptr, q_out, (hipStream_t)stream);
+}
+
+int dyllm_head_norm_rope_quant(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
+                               const dyllm_index_list *rows, int32_t B, int32_t L, dyllm_quant_cache *cache,
+                               void *q_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  if ((rc = check_quant(ctx, cache))) return rc;
+  return head_norm_rope(ctx, qkv, ld, g_q, g_k, rows, B, L, nullptr, cache, q_out, (hipStream_t)stream);
+}
+
+int dyllm_quant_write(dyllm_ctx *ctx, const void *k, const void *v, const dyllm_index_list *rows, int32_t B,
+                      int32_t L, dyllm_quant_cache *cache, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  Rows r;
+  if (!k || !v) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(k) || misaligned(v)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_quant(ctx, cache))) return rc;
+  if ((rc = check_rows(ctx, rows, B, L, false, &r))) return rc;
+  HeadsArgs a;
+  a.k = k; a.v = v; a.ld = (size_t)ctx->dkv;
+  a.rows = r; a.L = L; a.Hkv = ctx->cfg.n_kv_heads;
+  const int to = heads_to(&a, nullptr, cache);
+  launch_heads(dt(ctx), a, false, ctx->cfg.head_dim, to, (hipStream_t)stream);
+  return check_launch(ctx, "quant write");
+}
+
+int dyllm_quant_read(dyllm_ctx *ctx, const dyllm_quant_cache *cache, const dyllm_index_list *rows, int32_t B,
+                     int32_t L, void *k_out, void *v_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  Rows r;
+  if (!k_out || !v_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(k_out) || misaligned(v_out)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_quant(ctx, cache))) return rc;
+  if ((rc = check_rows(ctx, rows, B, L, false, &r))) return rc;
+  launch_quant_read(dt(ctx), quant_of(cache), cache->format, r, L, ctx->cfg.n_kv_heads, ctx->cfg.head_dim, k_out, v_out, (hipStream_t)stream);
+  return check_launch(ctx, "quant read");
+}
+
+int dyllm_partial_attention_quant(dyllm_ctx *ctx, const void *q_sal, const dyllm_quant_cache *cache,
+                                  const int32_t *kv_len, const dyllm_index_list *rows, int32_t B, int32_t L,
+                                  void *c_sal_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  Rows r;
+  if (!q_sal || !c_sal_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(q_sal) || misaligned(c_sal_out) || ((uintptr_t)kv_len & 3)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_quant(ctx, cache))) return rc;
+  if ((rc = check_rows(ctx, rows, B, L, false, &r))) return rc;
+  return enqueue_attention_quant(ctx, q_sal, cache, kv_len, r, rows ? rows->offsets : nullptr, B, L, c_sal_out, (hipStream_t)stream);
+}
+
+int dyllm_qkv_refresh_normed(dyllm_ctx *ctx, const dyllm_layer_weights *w, const void *g_q, const void *g_k,
+                             const void *x, const dyllm_index_list *rows, int32_t B, int32_t L,
+                             dyllm_layer_cache *cache, dyllm_quant_cache *quant, void *q_sal_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  Rows r;
+  if ((rc = check_weights(ctx, w, true, false))) return rc;
+  if (!x || !q_sal_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (!cache == !quant) return fail(ctx, DYLLM_ERR_INVALID_ARG, "exactly one of cache and quant is given");
+  if (quant && (rc = check_quant(ctx, quant))) return rc;
+  if (cache && (!cache->k || !cache->v)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "cache pointer is NULL");
+  if (misaligned(x) || misaligned(q_sal_out) || (cache && (misaligned(cache->k) || misaligned(cache->v))))
+    return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_gains(ctx, g_q, g_k))) return rc;
+  if ((rc = check_rows(ctx, rows, B, L, true, &r))) return rc;
+  return enqueue_qkv_normed(ctx, w, g_q, g_k, x, r, B, L, cache, quant, q_sal_out, (hipStream_t)stream);
+}
+
+int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const void *g_q, const void *g_k,
+                           dyllm_layer_cache *cache, dyllm_quant_cache *quant, const int32_t *kv_len, const void *x,
+                           const dyllm_index_list *idx_in, int32_t B, int32_t L, float tau,
+                           dyllm_index_list *idx_out, float *cos_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  hipStream_t s = (hipStream_t)stream;
+  if ((rc = check_bl(ctx, B, L))) return rc;
+  if ((rc = check_weights(ctx, w, true, true))) return rc;
+  if ((rc = check_quant(ctx, quant))) return rc;
+  if (!cache || !cache->c || !cache->out || !x) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (x == cache->out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "x aliases cache->out");
+  if (misaligned(x) || misaligned(cache->c) || misaligned(cache->out) || ((uintptr_t)kv_len & 3))
+    return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_gains(ctx, g_q, g_k))) return rc;
+  if ((rc = check_list(ctx, idx_in, "idx_in"))) return rc;
+  if ((rc = check_list(ctx, idx_out, "idx_out"))) return rc;
+  if ((idx_out->idx && idx_out->idx == idx_in->idx) || idx_out->offsets == idx_in->offsets)
+    return fail(ctx, DYLLM_ERR_INVALID_ARG, "idx_out aliases idx_in");
+  const Rows rin = rows_of(idx_in, B);
+  if ((rc = enqueue_qkv_normed(ctx, w, g_q, g_k, x, rin, B, L, nullptr, quant, ctx->qs, s))) return rc;
+  if ((rc = enqueue_attention_quant(ctx, ctx->qs, quant, kv_len, rin, idx_in->offsets, B, L, ctx->csal, s))) return rc;
+  launch_saliency(dt(ctx), ctx->csal, cache->c, rin, ctx->dq, tau, cos_out ? cos_out : ctx->cosb, ctx->flag, 1, s);
+  launch_compact(ctx->flag, rin, B, L, idx_out->idx, idx_out->offsets, idx_out->cap, ctx->status, ctx->scan, s);
+  if ((rc = check_launch(ctx, "saliency / compact"))) return rc;
+  Rows rout = rows_of(idx_out, B);  // (a subset of idx_in, whose capacity sizes the grids)
+  if (rout.cap > idx_in->cap) rout.cap = idx_in->cap;
+  return enqueue_ffn(ctx, w, x, cache->c, rout, cache->out, (size_t)B * L, s);
 }
 
 }  // extern "C"

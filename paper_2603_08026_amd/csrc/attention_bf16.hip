@@ -357,17 +357,6 @@ __global__ __launch_bounds__(64 * NW) void k_attn_bf16(AttnArgs a, int q_tiles) 
 //     other four -- every bank once (SQ_LDS_BANK_CONFLICT = 0; with p ^ (r % 8) both groups fell on
 //     the same four octets and every read took twice its cycles).
 
-// value of the lane 32 away combined with this lane's (v_permlane32_swap: no LDS round trip)
-__device__ __forceinline__ float xhalf_max(float x) {
-  const unsigned u = __float_as_uint(x);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float xhalf_sum(float x) {
-  const unsigned u = __float_as_uint(x);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 // sum over the 16 lanes of a row of lanes, in all of them (rotations inside the row: no LDS)
 __device__ __forceinline__ float row16_sum(float x) {
   x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false));

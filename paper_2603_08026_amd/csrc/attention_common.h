@@ -104,6 +104,17 @@ __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // last lane of row 1 -> rows 2 and 3
   return x;
 }
+// value of the lane 32 away combined with this lane's (v_permlane32_swap: no LDS round trip)
+__device__ __forceinline__ float xhalf_max(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float xhalf_sum(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 // Work item of a workgroup: sequence (or -1: no item), index of its first row in the row list, first packed row of the tile,
 // packed rows in it, whether the tile is its sequence's only one.
 struct AttnItem { int seq = -1, row = 0, packed = 0, n = 0, only = 0, kv_head = 0, split = 0; };

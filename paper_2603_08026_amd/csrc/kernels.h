@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "gemm_plan.h"
+#include "quant.h"
 
 namespace dy {
 
@@ -134,6 +135,26 @@ void launch_merge_compact(Rows a, Rows b, int pos_lo, uint8_t *flag_out, int B, 
                           int32_t *out_offsets, int out_cap, int32_t *status, int32_t *scan, hipStream_t s);
 constexpr int MERGE_TOKENS = 8192;
 
+// ---- heads of a row (headops.hip) -----------------------------------------------------------------
+// Row j of q, k, v (`ld` elements apart; T-typed, or fp32 sums of a raw GEMM result with the biases still to come) belongs to token row_j.
+// Query and key heads: RMSNorm with gain g_q / g_k (nullptr: none), rotation by the table entry of position row_j mod L (tab ==
+// nullptr: none).  q goes to q_out[j], k and v to row_j of the caches (to: 0 T-typed, 1 + format: codes).  H or Hkv may be 0.
+struct HeadsArgs {
+  const void *q = nullptr, *k = nullptr, *v = nullptr;
+  size_t ld = 0;
+  Splits splits;
+  const void *bq = nullptr, *bk = nullptr, *bv = nullptr, *g_q = nullptr, *g_k = nullptr;
+  float eps = 0.f;
+  const float *tab = nullptr;
+  Rows rows{};
+  int L = 0, H = 0, Hkv = 0;
+  void *q_out = nullptr, *kc = nullptr, *vc = nullptr;
+  QuantCache quant;
+};
+void launch_heads(DType t, const HeadsArgs &a, bool sums, int dh, int to, hipStream_t s);
+// k_out[j], v_out[j] = the cached rows row_j, code * scale rounded to T
+void launch_quant_read(DType t, const QuantCache &c, int format, Rows rows, int L, int Hkv, int dh, void *k_out, void *v_out, hipStream_t s);
+
 // ---- attention ---------------------------------------------------------------------------------
 struct AttnArgs {
   const void *q;        // [cap, H, dh] T-typed; with q_by_token: [T, H, dh], row of query j = rows.idx[j]
@@ -168,6 +189,15 @@ struct AttnArgs {
 };
 // attention rows; merges the splits into a.out unless a.partial is set
 void launch_attention(DType t, const AttnArgs &a, hipStream_t s);
+// exact rows over a cache of codes (a.q, a.rows, a.offsets and what attention_quant_plan left; a.k and a.v are not looked at):
+// sequence b has min(kv_len[b], L) keys (kv_len == nullptr: L), and rows without a key are zero.  Into a.out.
+struct QuantAttn {
+  QuantCache cache;
+  const int32_t *kv_len = nullptr;
+  int format = 0;
+};
+void launch_attention_quant(DType t, const AttnArgs &a, const QuantAttn &q, hipStream_t s);
+void attention_quant_plan(DType t, size_t part_elems, AttnArgs *a);
 // exact rows (a) and the context update of Alg. 4 (b: norm_k) in one launch, where both are bf16 with head_dim 128, one key split
 // and the same query tile: returns whether they were launched
 bool launch_attention_both(const AttnArgs &a, const AttnArgs &b, hipStream_t s);

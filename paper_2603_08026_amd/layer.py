@@ -28,13 +28,15 @@ def to_host(t: torch.Tensor) -> np.ndarray:
     return t.detach().float().cpu().numpy().astype(np.float64)
 
 
+CODES = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
 MATRICES = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down")
 
 
 class Layer:
     def __init__(self, hidden, n_heads, n_kv_heads, head_dim, ffn, dtype: str, batch: int, seq: int,
                  max_rows: int = 0, rms_eps: float = 1e-5, rope_theta: float = 10000.0, ctx=None,
-                 keep_lse: bool = False):
+                 keep_lse: bool = False, codes: Optional[str] = None):
+        """codes: None, or the format ("e4m3", "int8") of keys and values held in 8 bits (layer_step_quant)."""
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU: the dyllm library only runs on a HIP device")
         self.dtype = dtype
@@ -46,8 +48,12 @@ class Layer:
         self.ctx = B_.Context(self.cfg) if ctx is None else ctx  # layers of a stack share one
         td = torch_dtype(dtype)
         T = batch * seq
-        self.k = torch.zeros(batch, seq, n_kv_heads, head_dim, dtype=td, device="cuda")
-        self.v = torch.zeros_like(self.k)
+        self.quant = B_.QuantCache.empty(batch, seq, n_kv_heads, head_dim, CODES[codes]) if codes else None
+        if codes:
+            self.k = self.v = None
+        else:
+            self.k = torch.zeros(batch, seq, n_kv_heads, head_dim, dtype=td, device="cuda")
+            self.v = torch.zeros_like(self.k)
         self.c = torch.zeros(batch, seq, self.dq, dtype=td, device="cuda")
         self.out = torch.zeros(batch, seq, hidden, dtype=td, device="cuda")
         # optional fifth cache: log-normalisers of every token's last exact attention row (needed by the
@@ -59,11 +65,12 @@ class Layer:
         self.cos = torch.zeros(self.rows_cap, dtype=torch.float32, device="cuda")
         self.wt: Dict[str, torch.Tensor] = {}
         self.w = None
+        self.g_q = self.g_k = None  # gains of the query and key heads' norms (weights "g_q", "g_k"), layer_step_quant
 
     @classmethod
-    def from_shape(cls, shape, batch, seq, max_rows=0, ctx=None, keep_lse=False):
+    def from_shape(cls, shape, batch, seq, max_rows=0, ctx=None, keep_lse=False, codes=None):
         return cls(shape.hidden, shape.n_heads, shape.n_kv_heads, shape.head_dim, shape.ffn, shape.dtype,
-                   batch, seq, max_rows, shape.rms_eps, shape.rope_theta, ctx, keep_lse)
+                   batch, seq, max_rows, shape.rms_eps, shape.rope_theta, ctx, keep_lse, codes)
 
     def pack(self, t: torch.Tensor) -> torch.Tensor:
         """Row-major bf16 matrix -> a new tensor in the panel layout the bf16 kernels read (library call)."""
@@ -76,6 +83,7 @@ class Layer:
             wt = {n: (self.pack(t) if n in MATRICES else t) for n, t in wt.items()}
         self.wt = dict(wt)  # what the library reads (bf16: packed matrices)
         self.w = B_.make_weights(self.wt)
+        self.g_q, self.g_k = self.wt.get("g_q"), self.wt.get("g_k")
 
     def set_weights(self, w: Dict[str, np.ndarray]):
         """Row-major host weights [out, in]; bf16 layers re-lay the matrices on the device."""
@@ -93,6 +101,10 @@ class Layer:
             self.lse.copy_(torch.from_numpy(np.ascontiguousarray(caches["lse"], dtype=np.float32)).cuda())
 
     def get_caches(self) -> Dict[str, np.ndarray]:
+        if self.quant is not None:  # keys and values as they are read back
+            k, v = (torch.empty(self.B, self.L, self.Hkv, self.dh, dtype=torch_dtype(self.dtype), device="cuda") for _ in range(2))
+            self.ctx.quant_read(self.quant, None, self.B, self.L, k, v)
+            return {"k": to_host(k), "v": to_host(v), "c": to_host(self.c), "out": to_host(self.out)}
         return {n: to_host(getattr(self, n)) for n in ("k", "v", "c", "out")}
 
     def make_list(self, idx: np.ndarray, offsets: np.ndarray, cap: Optional[int] = None) -> B_.IndexList:
@@ -114,6 +126,15 @@ class Layer:
         out = self.idx_out if idx_out is None else idx_out
         self.ctx.layer_step(self.w, self.cache, x_dev, idx_in, self.B, self.L, tau, out,
                             self.cos if want_cos else None)
+        return out
+
+    def layer_step_quant(self, x_dev: torch.Tensor, idx_in: B_.IndexList, tau: float,
+                         idx_out: Optional[B_.IndexList] = None, want_cos: bool = True,
+                         kv_len: Optional[torch.Tensor] = None):
+        """A step of a layer made with `codes`; a list of all tokens with tau > 1 makes it a dense one.  kv_len: int32 [B] or None."""
+        out = self.idx_out if idx_out is None else idx_out
+        self.ctx.layer_step_quant(self.w, self.g_q, self.g_k, self.cache, self.quant, x_dev, idx_in, self.B, self.L, tau, out,
+                                  self.cos if want_cos else None, kv_len)
         return out
 
     def layer_step_approx(self, x_dev: torch.Tensor, idx_in: B_.IndexList, tau: float,
