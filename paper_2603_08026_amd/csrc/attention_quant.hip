@@ -16,48 +16,381 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
+// a pointer into global memory that all lanes agree on, in scalar registers
+template <typename P> using Global = __attribute__((address_space(1))) P *;
+template <typename P> __device__ __forceinline__ Global<P> uniform(P *p) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return (Global<P>)(((uint64_t)hi << 32) | lo);
+}
+
+// computed here, not where it is used (the compiler would sink it past a branch, away from the products it is to run under)
+template <typename V> __device__ __forceinline__ void here(V &v) { asm volatile("" : "+v"(v)); }
+
 // keys of sequence b
 __device__ __forceinline__ int keys_of(const QuantAttn &q, int L, int b) {
   return q.kv_len ? min(max(q.kv_len[b], 0), L) : L;
 }
 
-template <int DH_, int WQ_, int WK_> struct QTile {
-  static constexpr int DH = DH_, WQ = WQ_, WK = WK_, NW = WQ * WK, NT = 64 * NW;
-  static constexpr int BQ = 32 * WQ, TK = 32 * WK;
-  static constexpr int ROWB = DH * 2, REGION = TK * ROWB;
-  static constexpr int DB = DH / 32, KK = DH / 16, CH = DH / 16;  // CH: 16-byte chunks of codes in a key
-  static constexpr int PER = 2 * TK * CH / NT;                    // chunks per thread and tile
-  static constexpr int PER_WAVE = (DB * 16 + 2) * 64;
-  static constexpr int MERGE_BYTES = (WK - 1) * WQ * PER_WAVE * 4;
-  static constexpr int LDS = 2 * REGION > MERGE_BYTES ? 2 * REGION : MERGE_BYTES;
-  static_assert(PER >= 1 && PER * NT == 2 * TK * CH, "a tile is copied in whole chunks per thread");
-  // 16-byte chunk c of key row r, and 32-byte pair p of value row r, in a row of the stage
-  __device__ static __forceinline__ int k_chunk(int r, int c) { return DH == 128 ? c ^ (r & 15) : c ^ ((r >> 1) & 7); }
-  __device__ static __forceinline__ int v_pair(int r, int p) { return DH == 128 ? p ^ (2 * (r & 3)) : p ^ (2 * ((r >> 1) & 1)); }
+// un-normalised rows of a split.  One without a key counts for nothing; where all are without one, the first makes the row zero
+template <int DH>
+__device__ __forceinline__ void store_partial(const AttnArgs &a, const floatx16 (&acc_o)[DH / 32], int split, uint32_t place, int lhi, bool none,
+                                              float m_run, float l_run) {
+  const size_t at = (size_t)split * a.rows.cap * a.H + place;
+  float *po = a.part_o + at * DH + 4 * lhi;
+#pragma unroll
+  for (int db = 0; db < DH / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4 *>(po + db * 32 + 8 * g) = float4{acc_o[db][4 * g], acc_o[db][4 * g + 1], acc_o[db][4 * g + 2], acc_o[db][4 * g + 3]};
+  if (lhi == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = float2{none && split == 0 ? 0.f : m_run * LN2, none && split == 0 ? 1.f : l_run};
+}
+
+template <int DH_> struct STile {
+  static constexpr int DH = DH_, NW = 4, NS = 2;
+  static constexpr int BQ = 32, TK = 32;                        // query rows, keys of a wave's tile
+  static constexpr int CH = DH / 16, RPC = 1024 / DH;           // 16-byte chunks of a key, keys of a copy
+  static constexpr int RAW = TK * DH, COPIES = RAW / 1024;      // codes of K (and of V)
+  static constexpr int STAGE = 2 * RAW + 8 * TK, PER_TILE = 2 * COPIES + 1;
+  static constexpr int DB = DH / 32, KK = DH / 16, WORDS = 2 * KK;
+  static constexpr int PER_WAVE = (DB * 16 + 2) * 64;           // floats of a wave's result
+  static constexpr int RING = NS * STAGE, LDS = NW * RING;
+  static_assert((NS - 1) * PER_TILE < 64 && (NW - 1) * PER_WAVE * 4 <= LDS, "vmcnt immediate, merge scratch");
+  // position of 16-byte chunk c of row r: the rows that a read serves at a time cover all banks once
+  __device__ static __forceinline__ int k_chunk(int r, int c) { return DH == 128 ? c ^ ((r >> 1) & 7) : c ^ ((r >> 2) & 3); }
+  __device__ static __forceinline__ int v_chunk(int r, int c) {
+    return DH == 128 ? c ^ (2 * ((r >> 1) & 1) + 4 * ((r >> 3) & 1)) : c ^ (2 * ((r >> 3) & 1));
+  }
 };
 
-template <int DH, int WQ, int WK, int F>
-__global__ __launch_bounds__(64 * WQ * WK) void k_attn_quant(AttnArgs a, QuantAttn qc, int q_tiles) {
-  using T = QTile<DH, WQ, WK>;
-  constexpr int TK = T::TK, ROWB = T::ROWB, DB = T::DB, KK = T::KK, CH = T::CH, PER = T::PER, NT = T::NT;
+template <int DH, int F>
+__global__ __launch_bounds__(256, 2) void k_attn_quant_stream(AttnArgs a, QuantAttn qc, int q_tiles) {
+  using T = STile<DH>;
+  typedef int intx2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) intx2 lds_intx2;
+  constexpr int TK = T::TK, DB = T::DB, KK = T::KK, CH = T::CH, NW = T::NW, NS = T::NS, WORDS = T::WORDS;
   __shared__ __align__(1024) unsigned char smem[T::LDS];
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int l32 = lane % 32, lhi = lane / 32;
-  const int wq = wave / WK, wk = wave % WK;
   const AttnItem item = attn_work_item_grouped(a, T::BQ, q_tiles, blockIdx.x);
   const int b = item.seq, kvh = item.kv_head, split = item.split;
   if (b < 0) return;  // uniform: no such tile
   const int nq = item.n, grp = a.H / a.Hkv;
-  int jq, hq;
+  uint32_t place;  // row * H + head of this lane's query (rows past the end: the last one again, their results are never stored)
   {
-    int r = wq * 32 + l32;
-    r = r < nq ? r : nq - 1;
-    const int p = item.packed + r;
+    const int p = item.packed + min(l32, nq - 1);
+    place = (uint32_t)(item.row + p / grp) * (uint32_t)a.H + (uint32_t)(kvh * grp + p % grp);
+  }
+  const int Lk = keys_of(qc, a.L, b);
+  const int k_lo = min(split * a.chunk, Lk), k_hi = min(Lk, k_lo + a.chunk);
+  const int tiles = (k_hi - k_lo + TK - 1) / TK, n_tiles = tiles > wave ? (tiles - wave + NW - 1) / NW : 0;  // this wave's: wave, wave + 4, ..
+
+  // Copies of codes and scales, tile by tile, into the wave's own ring.
+  unsigned char *own = smem + wave * T::RING;
+  const uint32_t lds0 = lds_offset_of(own);
+  const uint32_t stride = (uint32_t)a.Hkv * DH;
+  const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH, first_s = ((size_t)b * a.Hkv + kvh) * a.L;
+  const uint8_t *kc = (const uint8_t *)uniform(qc.cache.k + first), *vc = (const uint8_t *)uniform(qc.cache.v + first);
+  const float *src_s = (lhi ? qc.cache.vs : qc.cache.ks) + first_s;
+  uint32_t off_k[T::COPIES], off_v[T::COPIES];  // of a full tile
+  auto offset = [&](int i, int last, int v) {
+    const int row = i * T::RPC + lane / CH, p = lane % CH;
+    return (uint32_t)min(row, last) * stride + (v ? T::v_chunk(row, p) : T::k_chunk(row, p)) * 16u;
+  };
+#pragma unroll
+  for (int i = 0; i < T::COPIES; ++i) {
+    off_k[i] = offset(i, TK - 1, 0);
+    off_v[i] = offset(i, TK - 1, 1);
+  }
+  // full: all of the tile's keys exist; else those past the end are the last one again, masked later
+  auto issue = [&](int n, auto full_c) {
+    constexpr bool FULL = decltype(full_c)::value;
+    const uint32_t base = lds0 + (uint32_t)(n % NS) * T::STAGE;
+    const int k0 = k_lo + (wave + n * NW) * TK, last = min(k_hi - 1 - k0, TK - 1);
+    const uint8_t *k = kc + (size_t)k0 * stride, *v = vc + (size_t)k0 * stride;
+#pragma unroll
+    for (int i = 0; i < T::COPIES; ++i) {
+      dma16_s(k, FULL ? off_k[i] : offset(i, last, 0), base + i * 1024u);
+      dma16_s(v, FULL ? off_v[i] : offset(i, last, 1), base + T::RAW + i * 1024u);
+    }
+    dma4(src_s + k0 + (FULL ? l32 : min(l32, last)), base + 2 * T::RAW);
+  };
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+    if (s < n_tiles) issue(s, std::false_type{});
+
+  // (a lane holds the elements of the chunks that it reads of a key: those of half the head, CH / 2 neighbouring chunks)
+  bf16x8 qf[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8 *>((const bf16_t *)a.q + (size_t)place * DH + lhi * (DH / 2) + kk * 8);
+  floatx16 acc_o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc_o[db][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  const float sc = LOG2E / sqrtf((float)DH);  // scores are kept in the log2 domain
+  const int j8 = (lane % 16) / 2, hb = (lane / 16) & 1;
+  const int vrow = 4 * lhi + j8 % 4 + 8 * (j8 / 4);  // (+ 16 of the second step)
+
+  if (n_tiles > 0) {
+    uint4 kr[KK / 2];   // codes of K, and the scale of this lane's key
+    intx2 vr[2][DB];    // codes of V, transposed
+    float kscale = 0.f;
+    bf16x8 kf[KK], vf[2][DB], pf[2];
+    floatx16 s_cur, s_next;
+    auto stage = [&](int n) { return own + (n % NS) * T::STAGE; };
+    auto read_k = [&](int n) {
+      const unsigned char *st = stage(n);
+#pragma unroll
+      for (int i = 0; i < KK / 2; ++i) kr[i] = *reinterpret_cast<const uint4 *>(st + l32 * DH + T::k_chunk(l32, lhi * (CH / 2) + i) * 16);
+      if (F == Q_E4M3) kscale = *reinterpret_cast<const float *>(st + 2 * T::RAW + 4 * l32);
+    };
+    auto read_v = [&](int n) {
+      const unsigned char *st = stage(n);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const int row = vrow + 16 * k;
+          vr[k][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_intx2 *)(st + T::RAW + row * DH + T::v_chunk(row, 2 * db + hb) * 16 + 8 * (lane % 2)));
+        }
+    };
+    // a word of four codes to half an operand
+    auto convert_k = [&](int w) {
+      const uint32_t word = w % 4 == 0 ? kr[w / 4].x : w % 4 == 1 ? kr[w / 4].y : w % 4 == 2 ? kr[w / 4].z : kr[w / 4].w;
+      const uint2 r = q_bf16<F>(word, kscale);
+      uint4 u = __builtin_bit_cast(uint4, kf[w / 2]);
+      if (w % 2) { u.z = r.x; u.w = r.y; } else { u.x = r.x; u.y = r.y; }
+      kf[w / 2] = __builtin_bit_cast(bf16x8, u);
+    };
+    auto convert_v = [&](int w) {
+      const int k = w / (2 * DB), db = w / 2 % DB;
+      const uint2 r = q_bf16<F>((uint32_t)(w % 2 ? vr[k][db].y : vr[k][db].x), 1.f);
+      uint4 u = __builtin_bit_cast(uint4, vf[k][db]);
+      if (w % 2) { u.z = r.x; u.w = r.y; } else { u.x = r.x; u.y = r.y; }
+      vf[k][db] = __builtin_bit_cast(bf16x8, u);
+    };
+    auto pv = [&](int i) { acc_o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i / DB][i % DB], pf[i / DB], acc_o[i % DB], 0, 0, 0); };
+    auto qk = [&](int kk) { s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], s_next, 0, 0, 0); };
+
+    // scores of the first tile
+    if (NS < n_tiles + 1) wait_vmcnt<(NS - 1) * T::PER_TILE>();
+    else wait_vmcnt<0>();
+    read_k(0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s_next[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[k][e] = (__bf16)0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vf[k][db] = pf[k];
+    }
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) convert_k(w);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qk(kk);
+    s_cur = s_next;
+
+    // Tile n: P V of tile n - 1 while half of tile n's exponentials are taken and K of tile n + 1 is converted, then the scores of tile
+    // n + 1 while the other half are taken and V of tile n is converted.
+    auto body = [&](int n, auto steady_c) {
+      constexpr bool STEADY = decltype(steady_c)::value;
+      if (STEADY || n + NS - 1 < n_tiles) wait_vmcnt<(NS - 2) * T::PER_TILE>();  // tile n + 1 has landed
+      else wait_vmcnt<0>();
+      read_k(n + 1);  // (behind the last tile: a stage that holds none, whose scores are dropped)
+      read_v(n);
+      const int k0 = k_lo + (wave + n * NW) * TK;
+      const unsigned char *scales = stage(n) + 2 * T::RAW + 16 * lhi;
+      float vscale[16];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 v4 = *reinterpret_cast<const float4 *>(scales + 4 * TK + 32 * g);
+        vscale[4 * g] = v4.x; vscale[4 * g + 1] = v4.y; vscale[4 * g + 2] = v4.z; vscale[4 * g + 3] = v4.w;
+        if (F == Q_INT8) {
+          const float4 k4 = *reinterpret_cast<const float4 *>(scales + 32 * g);
+          s_cur[4 * g] *= k4.x; s_cur[4 * g + 1] *= k4.y; s_cur[4 * g + 2] *= k4.z; s_cur[4 * g + 3] *= k4.w;
+        }
+      }
+      if (!STEADY && k0 + TK > k_hi) {  // uniform: only the last tile can hold keys past the end
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (k0 + 4 * lhi + 8 * (e / 4) + (e % 4) >= k_hi) s_cur[e] = -INFINITY;
+      }
+      float mx = s_cur[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s_cur[e]);
+      mx = xhalf_max(mx) * sc;
+      // the running reference moves where the maximum exceeds it by more than 2^8: rare after the first tiles
+      const bool need = mx > m_run + 8.0f;
+      if (__any(need)) {
+        const float corr = need ? __builtin_amdgcn_exp2f(m_run - mx) : 1.0f;
+        m_run = need ? mx : m_run;
+        l_run *= corr;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc_o[db][e] *= corr;
+        // the last tile's probabilities, whose products are still to come, belong to the old reference
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint4 w = __builtin_bit_cast(uint4, pf[k]);
+          const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+          uint32_t o[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) o[q] = pack_bf16(__uint_as_float(ww[q] << 16) * corr, __uint_as_float(ww[q] & 0xffff0000u) * corr);
+          pf[k] = __builtin_bit_cast(bf16x8, uint4{o[0], o[1], o[2], o[3]});
+        }
+      }
+      const float neg_ref = m_run == -INFINITY ? 0.f : -m_run;
+      float pe[16];
+      uint32_t pw[8];
+      // the scale of the value joins the probability ahead of its one rounding; the sum is over what there was before
+      auto round_pair = [&](int i) {
+        l_run += pe[2 * i] + pe[2 * i + 1];
+        pw[i] = pack_bf16(pe[2 * i] * vscale[2 * i], pe[2 * i + 1] * vscale[2 * i + 1]);
+      };
+      auto upto = [](int slot) { return slot < 0 ? 0 : 8 * (slot + 1) / KK; };  // exponentials of a phase taken by then
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int phase = 0; phase < 2; ++phase) {
+        if (phase == 1) {
+          if (STEADY || n + NS < n_tiles) {
+            wait_lgkmcnt0();  // tile n has been read: another may come in its place
+            issue(n + NS, steady_c);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s_next[e] = 0.f;
+        }
+#pragma unroll
+        for (int slot = 0; slot < KK; ++slot) {
+          if (phase == 0) pv(slot); else qk(slot);
+#pragma unroll
+          for (int w = WORDS * slot / KK; w < WORDS * (slot + 1) / KK; ++w)
+            if (phase == 0) convert_k(w); else convert_v(w);
+#pragma unroll
+          for (int g = 8 * phase + upto(slot - 1); g < 8 * phase + upto(slot); ++g) {
+            pe[g] = __builtin_amdgcn_exp2f(fmaf(s_cur[g], sc, neg_ref));
+            here(pe[g]);
+          }
+          if (slot > 0) {
+#pragma unroll
+            for (int i = (8 * phase + upto(slot - 2)) / 2; i < (8 * phase + upto(slot - 1)) / 2; ++i) round_pair(i);
+          } else if (phase == 1) {
+#pragma unroll
+            for (int i = upto(KK - 2) / 2; i < 4; ++i) round_pair(i);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int i = (8 + upto(KK - 2)) / 2; i < 8; ++i) round_pair(i);
+      pf[0] = __builtin_bit_cast(bf16x8, uint4{pw[0], pw[1], pw[2], pw[3]});
+      pf[1] = __builtin_bit_cast(bf16x8, uint4{pw[4], pw[5], pw[6], pw[7]});
+      s_cur = s_next;
+    };
+    int n = 0;
+    for (; n + NS + 1 < n_tiles; ++n) body(n, std::true_type{});  // (each with a tile to copy that is not the wave's last)
+    for (; n < n_tiles; ++n) body(n, std::false_type{});
+#pragma unroll
+    for (int i = 0; i < KK; ++i) pv(i);  // the last tile's
+    l_run = xhalf_sum(l_run);
+  }
+
+  // merge of the waves through LDS
+  float *mg = reinterpret_cast<float *>(smem);
+  __syncthreads();
+  if (wave > 0) {
+    float *dst = mg + (size_t)(wave - 1) * T::PER_WAVE + lane;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dst[(db * 16 + e) * 64] = acc_o[db][e];
+    dst[(DB * 16) * 64] = m_run;
+    dst[(DB * 16 + 1) * 64] = l_run;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float M = m_run;
+#pragma unroll
+  for (int w = 1; w < NW; ++w) M = fmaxf(M, mg[(size_t)(w - 1) * T::PER_WAVE + (DB * 16) * 64 + lane]);
+  const float Ms = (M == -INFINITY) ? 0.f : M;
+  const float c0 = __builtin_amdgcn_exp2f(m_run - Ms);
+  l_run *= c0;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc_o[db][e] *= c0;
+#pragma unroll
+  for (int w = 1; w < NW; ++w) {
+    const float *src = mg + (size_t)(w - 1) * T::PER_WAVE + lane;
+    const float cw = __builtin_amdgcn_exp2f(src[(DB * 16) * 64] - Ms);
+    l_run = fmaf(src[(DB * 16 + 1) * 64], cw, l_run);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc_o[db][e] = fmaf(src[(db * 16 + e) * 64], cw, acc_o[db][e]);
+  }
+  if (l32 >= nq) return;
+  if (a.splits > 1) {
+    store_partial<DH>(a, acc_o, split, place, lhi, tiles == 0, M, l_run);
+    return;
+  }
+  const float inv = tiles > 0 ? 1.0f / l_run : 0.f;  // (a sequence without keys: zeros)
+  bf16_t *out = (bf16_t *)a.out + (size_t)place * DH + 4 * lhi;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2 *>(out + db * 32 + 8 * g) =
+          uint2{pack_bf16(acc_o[db][4 * g] * inv, acc_o[db][4 * g + 1] * inv), pack_bf16(acc_o[db][4 * g + 2] * inv, acc_o[db][4 * g + 3] * inv)};
+}
+
+template <int DH> void launch_stream(const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
+  using T = STile<DH>;
+  const int q_tiles = max_q_tiles_grouped(a, T::BQ), grid = attn_grid_grouped(a, q_tiles);
+  if (q.format == Q_E4M3) k_attn_quant_stream<DH, Q_E4M3><<<grid, 256, 0, s>>>(a, q, q_tiles);
+  else k_attn_quant_stream<DH, Q_INT8><<<grid, 256, 0, s>>>(a, q, q_tiles);
+}
+
+// ---- 128 query rows a workgroup ------------------------------------------------------------------------
+template <int DH_, int NW_> struct QTile {
+  static constexpr int DH = DH_, NW = NW_, NT = 64 * NW, BQ = 32 * NW, TK = 32;
+  static constexpr int ROWB = DH * 2, ROWK = ROWB + 16;             // bytes of a converted row; of K with a gap, so that a lane's reads differ by constants
+  static constexpr int HOT_K = TK * ROWK, HOT = TK * ROWB;
+  static constexpr int NK = 2, NV = 3, NR = NW == 8 ? 6 : 3, CYCLE = 6;  // converted K and V, tiles of codes and their scales; all repeat after CYCLE
+  static constexpr int RAW = 2 * TK * DH;                           // a tile of codes: K and V, in the order of the lanes that copy them
+  static constexpr int PER = 2 * TK * DH / (NT * 16);               // 16-byte chunks of codes, a lane's share of a tile
+  static constexpr int AT_K = 0, AT_V = NK * HOT_K, AT_RAW = AT_V + NV * HOT, AT_RS = AT_RAW + NR * RAW, AT_SC = AT_RS + NR * NW * 256, LDS = AT_SC + NV * 8 * TK;
+  static constexpr int DB = DH / 32, KK = DH / 16, SLOTS = DB + KK;
+  static constexpr int WORDS = 4 * PER;                             // of codes, a lane's share of a tile
+  static_assert(PER >= 1 && PER * NT * 16 == 2 * TK * DH && LDS <= (NW == 8 ? 160 : 80) * 1024 && BQ * ROWB <= LDS,
+                "eight waves to a CU; the rows leave by way of the same memory");
+  // 32-byte pair p of value row r: the rows that a read serves at a time cover all banks once
+  __device__ static __forceinline__ int v_pair(int r, int p) { return DH == 128 ? p ^ (2 * (r & 3)) : p ^ (2 * ((r >> 1) & 1)); }
+};
+
+template <int DH, int F, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, QuantAttn qc, int q_tiles) {
+  using T = QTile<DH, NW>;
+  constexpr int TK = T::TK, ROWB = T::ROWB, DB = T::DB, KK = T::KK, PER = T::PER, SLOTS = T::SLOTS, WORDS = T::WORDS;
+  __shared__ __align__(1024) unsigned char smem[T::LDS];
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+  const int l32 = lane % 32, lhi = lane / 32;
+  const AttnItem item = attn_work_item_grouped(a, T::BQ, q_tiles, blockIdx.x);
+  const int b = item.seq, kvh = item.kv_head, split = item.split;
+  if (b < 0) return;  // uniform: no such tile
+  const int nq = item.n, grp = a.H / a.Hkv;
+  int jq, hq;  // this lane's query (rows past the end: the last one again, their results are never stored)
+  {
+    const int p = item.packed + min(wave * 32 + l32, nq - 1);
     jq = item.row + p / grp;
     hq = kvh * grp + p % grp;
   }
   const int Lk = keys_of(qc, a.L, b);
   const int k_lo = min(split * a.chunk, Lk), k_hi = min(Lk, k_lo + a.chunk);
+  const int n_tiles = (k_hi - k_lo + TK - 1) / TK;
 
   bf16x8 qf[KK];
   {
@@ -71,166 +404,378 @@ __global__ __launch_bounds__(64 * WQ * WK) void k_attn_quant(AttnArgs a, QuantAt
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc_o[db][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  const float sc = LOG2E / sqrtf((float)DH);
+  const float sc = LOG2E / sqrtf((float)DH);  // scores are kept in the log2 domain
 
+  // Copies: a wave copies the codes of 8 keys of a tile and their scales, lane by lane where the same lane reads them, so that its own wait
+  // is enough.  A lane's chunk: key own_key, codes 16 own_c and on, of K or of V.  (The halves of an odd key's V change places:
+  // neighbouring keys then write to other banks.)
+  const uint32_t lds0 = lds_offset_of(smem);
   const size_t stride = (size_t)a.Hkv * DH;
   const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH, first_s = ((size_t)b * a.Hkv + kvh) * a.L;
+  auto own_v = [&](int u) { return PER == 2 ? u : DH == 128 ? wave / (NW / 2) : lane / 32; };
+  const int own_8 = DH == 128 && PER == 1 ? wave % (NW / 2) : wave;  // the keys 8 own_8 .. of a tile
+  const int own_key = own_8 * 8 + (DH == 128 ? lane / 8 : (lane % 32) / 4), own_c = DH == 128 ? lane % 8 : lane % 4;
+  const uint8_t *kc = (const uint8_t *)uniform(qc.cache.k + first), *vc = (const uint8_t *)uniform(qc.cache.v + first);
+  const uint8_t *code_at[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) code_at[u] = DH == 128 ? (const uint8_t *)uniform((own_v(u) ? qc.cache.v : qc.cache.k) + first) : nullptr;
+  const float *src_s = (lane & 8 ? qc.cache.vs : qc.cache.ks) + first_s;  // (8 scales of K, 8 of V, the same again)
+  const int scale_key = own_8 * 8 + lane % 8;
+  const uint32_t off_full = (uint32_t)own_key * (uint32_t)stride + own_c * 16u;
+  // full: all of the tile's keys exist; else those past the end are the last one again, masked later
+  auto issue = [&](int t, auto st_c, auto full_c) {
+    constexpr int ST = decltype(st_c)::value;
+    constexpr bool FULL = decltype(full_c)::value;
+    const uint32_t base = lds0 + T::AT_RAW + (ST % T::NR) * T::RAW + (uint32_t)wave * (PER * 1024u);
+    const int k0 = k_lo + t * TK, last = k_hi - 1 - k0;
+    const uint32_t off = FULL ? off_full : (uint32_t)min(own_key, last) * (uint32_t)stride + own_c * 16u;
+    if constexpr (DH == 128) {
+#pragma unroll
+      for (int u = 0; u < PER; ++u) dma16_s(code_at[u] + (size_t)k0 * stride, off, base + u * 1024u);
+    } else {
+      dma16((lhi ? vc : kc) + (size_t)k0 * stride + off, base);
+    }
+    dma4(src_s + k0 + (FULL ? scale_key : min(scale_key, last)), lds0 + T::AT_RS + (ST % T::NR) * (NW * 256u) + wave * 256u);
+  };
+  auto wait_tiles = [&](auto left_c) { wait_vmcnt<decltype(left_c)::value * (PER + 1)>(); };  // all but the youngest tiles have landed
+  auto hot_k = [&](int st) { return smem + T::AT_K + (st % T::NK) * T::HOT_K; };
+  auto hot_v = [&](int st) { return smem + T::AT_V + (st % T::NV) * T::HOT; };
+  // Conversion: this lane's chunks of a tile, a word of four codes at a time; every second word ends 16 bytes of bf16.
   uint4 raw[PER];
-  float scale[PER];
-  auto load = [&](int k0) {  // (keys past the end: the last one again, masked later)
+  float rs[PER];
+  auto read_raw = [&](auto st_c) {
+    constexpr int ST = decltype(st_c)::value;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const int i = tid + NT * u, isv = i / (TK * CH), in = i % (TK * CH);
-      const int key = min(k0 + in / CH, k_hi - 1);
-      raw[u] = *reinterpret_cast<const uint4 *>((isv ? qc.cache.v : qc.cache.k) + first + (size_t)key * stride + (in % CH) * 16);
-      scale[u] = (isv ? qc.cache.vs : qc.cache.ks)[first_s + key];
+      raw[u] = *reinterpret_cast<const uint4 *>(smem + T::AT_RAW + (ST % T::NR) * T::RAW + wave * (PER * 1024) + u * 1024 + lane * 16);
+      rs[u] = *reinterpret_cast<const float *>(smem + T::AT_RS + (ST % T::NR) * (NW * 256) + wave * 256 + own_v(u) * 32 + (own_key % 8) * 4);
     }
   };
-  auto store = [&]() {
+  int own_at[PER];
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int i = tid + NT * u, isv = i / (TK * CH), in = i % (TK * CH);
-      const int key = in / CH, c = in % CH;
-      const uint2 w0 = q_bf16<F>(raw[u].x, scale[u]), w1 = q_bf16<F>(raw[u].y, scale[u]);
-      const uint2 w2 = q_bf16<F>(raw[u].z, scale[u]), w3 = q_bf16<F>(raw[u].w, scale[u]);
-      unsigned char *row = smem + (isv ? T::REGION : 0) + key * ROWB;
-      const int c0 = isv ? 2 * T::v_pair(key, c) : T::k_chunk(key, 2 * c), c1 = isv ? c0 + 1 : T::k_chunk(key, 2 * c + 1);
-      *reinterpret_cast<uint4 *>(row + c0 * 16) = uint4{w0.x, w0.y, w1.x, w1.y};
-      *reinterpret_cast<uint4 *>(row + c1 * 16) = uint4{w2.x, w2.y, w3.x, w3.y};
+  for (int u = 0; u < PER; ++u) own_at[u] = own_v(u) ? own_key * ROWB + T::v_pair(own_key, own_c) * 32 : own_key * T::ROWK + own_c * 32;
+  uint2 even{};
+  auto convert = [&](int w, auto st_c) {
+    constexpr int ST = decltype(st_c)::value;
+    const int u = w / 4, i = w % 4, v = own_v(u);
+    const uint32_t word = i == 0 ? raw[u].x : i == 1 ? raw[u].y : i == 2 ? raw[u].z : raw[u].w;
+    const uint2 r = q_bf16<F>(word, rs[u]);
+    if (i % 2 == 0) {
+      even = r;
+    } else {
+      const int stage = v ? T::AT_V + (ST % T::NV) * T::HOT : T::AT_K + (ST % T::NK) * T::HOT_K;
+      *reinterpret_cast<uint4 *>(smem + stage + own_at[u] + i / 2 * 16) = uint4{even.x, even.y, r.x, r.y};
+      if (F == Q_INT8 && i == 3) *reinterpret_cast<float *>(smem + T::AT_SC + (ST % T::NV) * (8 * TK) + v * 4 * TK + own_key * 4) = rs[u];
     }
   };
+  auto convert_all = [&](auto st_c) {
+    read_raw(st_c);
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) convert(w, st_c);
+  };
+  auto barrier = []() {  // (copies that are under way stay so; the wait is one that the compiler knows of)
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+  };
+  constexpr int NR = T::NR;
+  using part = std::false_type;
+  auto first_tile = [&](auto st_c) {
+    constexpr int ST = decltype(st_c)::value;
+    if constexpr (ST < NR)
+      if (ST < n_tiles) issue(ST, st_c, part{});
+  };
+  first_tile(std::integral_constant<int, 0>{});
+  first_tile(std::integral_constant<int, 1>{});
+  first_tile(std::integral_constant<int, 2>{});
+  first_tile(std::integral_constant<int, 3>{});
+  first_tile(std::integral_constant<int, 4>{});
+  first_tile(std::integral_constant<int, 5>{});
+  // tile t has landed, of those up to t + ahead that exist
+  auto landed = [&](int t, auto ahead_c) {
+    constexpr int AHEAD = decltype(ahead_c)::value;
+    if (t + AHEAD < n_tiles) wait_tiles(ahead_c);
+    else if (AHEAD > 2 && t + 2 < n_tiles) wait_tiles(std::integral_constant<int, 2>{});
+    else wait_tiles(std::integral_constant<int, 0>{});
+  };
+  landed(1, std::integral_constant<int, NR - 2>{});
+  if (0 < n_tiles) convert_all(std::integral_constant<int, 0>{});
+  if (1 < n_tiles) convert_all(std::integral_constant<int, 1>{});
+  wait_lgkmcnt0();
+  if (NR < n_tiles) issue(NR, std::integral_constant<int, NR>{}, part{});
+  if (NR + 1 < n_tiles) issue(NR + 1, std::integral_constant<int, NR + 1>{}, part{});
+  barrier();
+  const int vrow = 4 * lhi + (lane % 16) / 4, hb = (lane / 16) & 1;
 
-  const int krow = wk * 32 + l32;
-  const int vrow = wk * 32 + 4 * lhi + (lane % 16) / 4, hb = (lane / 16) & 1;
-  if (k_lo < k_hi) load(k_lo);
-  for (int k0 = k_lo; k0 < k_hi; k0 += TK) {
-    __syncthreads();
-    store();
-    __syncthreads();
-    if (k0 + TK < k_hi) load(k0 + TK);
-    floatx16 s;
+  // tile t of place ST of the cycle, for t = 0 .. n - 1, as often as the cycle fits
+  auto cycles = [&](int &t, int n, auto &&each) {
+    for (; t < n; t += T::CYCLE) {
+      each(t, std::integral_constant<int, 0>{});
+      if (t + 1 < n) each(t + 1, std::integral_constant<int, 1>{});
+      if (t + 2 < n) each(t + 2, std::integral_constant<int, 2>{});
+      if (t + 3 < n) each(t + 3, std::integral_constant<int, 3>{});
+      if (t + 4 < n) each(t + 4, std::integral_constant<int, 4>{});
+      if (t + 5 < n) each(t + 5, std::integral_constant<int, 5>{});
+    }
+  };
+  if (wave * 32 >= nq) {  // uniform: a wave without a query converts its share
+    int t0 = 0;
+    cycles(t0, n_tiles, [&](int t, auto st_c) {
+      constexpr int ST = decltype(st_c)::value;
+      landed(t + 2, std::integral_constant<int, NR - 1>{});
+      barrier();
+      if (t + 2 < n_tiles) convert_all(std::integral_constant<int, ST + 2>{});
+      wait_lgkmcnt0();
+      if (t + 2 + NR < n_tiles) issue(t + 2 + NR, std::integral_constant<int, ST + 2 + NR>{}, part{});
+    });
+  } else if (n_tiles > 0) {
+    // While the vector ALU takes the exponentials of tile t and converts tile t + 2, the matrix pipe works through P V of tile t - 1 and
+    // the scores of tile t + 1.
+    floatx16 s_cur;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    for (int e = 0; e < 16; ++e) s_cur[e] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(smem + krow * ROWB + T::k_chunk(krow, 2 * kk + lhi) * 16);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], s, 0, 0, 0);
+      const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(hot_k(0) + l32 * T::ROWK + lhi * 16 + kk * 32);
+      s_cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], s_cur, 0, 0, 0);
     }
-    if (k0 + TK > k_hi) {  // uniform
-      const int key_base = k0 + wk * 32 + 4 * lhi;
+    bf16x8 vf[2][DB], pf[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (key_base + 8 * (e / 4) + (e % 4) >= k_hi) s[e] = -INFINITY;
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pf[ks][e] = (__bf16)0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vf[ks][db] = pf[ks];
     }
-    float mx = s[0];
+    auto pv = [&](int ks, int db) {  // O^T += V^T P^T of the tile held in vf / pf
+      acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][db], pf[ks], acc_o[db], 0, 0, 0);
+    };
+    auto body = [&](int t, auto steady_c, auto stage_c) {
+      constexpr bool STEADY = decltype(steady_c)::value;
+      constexpr int ST = decltype(stage_c)::value;
+      if (STEADY) wait_tiles(std::integral_constant<int, NR - 1>{});
+      else landed(t + 2, std::integral_constant<int, NR - 1>{});
+      barrier();  // K of tile t + 1 and V of tile t are converted
+      const bool more = STEADY || t + 2 < n_tiles;
+      if (more) read_raw(std::integral_constant<int, ST + 2>{});
+      const unsigned char *kt = hot_k(ST + 1), *vt = hot_v(ST);
+      bf16x8 kf[KK / 2];
+      auto read_k = [&](int kk) { kf[kk % (KK / 2)] = *reinterpret_cast<const bf16x8 *>(kt + l32 * T::ROWK + lhi * 16 + kk * 32); };
+      auto read_v = [&](int ks, int db) {
+        const unsigned char *p = vt + vrow * ROWB + 8 * (lane % 4) + ks * 16 * ROWB + T::v_pair(vrow, db * 2 + hb) * 32;
+        const shortx4 g0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p));
+        const shortx4 g1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + 8 * ROWB));
+        vf[ks][db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      const int k0 = k_lo + t * TK;
+      const unsigned char *scales = smem + T::AT_SC + (ST % T::NV) * (8 * TK) + 16 * lhi;  // (int8)
+      if constexpr (F == Q_INT8) {
 #pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-    mx = xhalf_max(mx) * sc;
-    const bool need = mx > m_run + 8.0f;
-    if (__any(need)) {
-      const float corr = need ? __builtin_amdgcn_exp2f(m_run - mx) : 1.0f;
-      m_run = need ? mx : m_run;
-      l_run *= corr;
+        for (int g = 0; g < 4; ++g) {
+          const float4 k4 = *reinterpret_cast<const float4 *>(scales + 32 * g);
+          s_cur[4 * g] *= k4.x; s_cur[4 * g + 1] *= k4.y; s_cur[4 * g + 2] *= k4.z; s_cur[4 * g + 3] *= k4.w;
+        }
+      }
+      if (!STEADY && k0 + TK > k_hi) {  // uniform: only the last tile can hold keys past the end
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+        for (int e = 0; e < 16; ++e)
+          if (k0 + 4 * lhi + 8 * (e / 4) + (e % 4) >= k_hi) s_cur[e] = -INFINITY;
+      }
+      auto convert_at = [&](int product) {  // behind the first twelve of sixteen products, so that all is written well ahead of the barrier
+        constexpr int OVER = 3 * DB;
+        if (more && product < OVER) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc_o[db][e] *= corr;
+          for (int w = product * WORDS / OVER; w < (product + 1) * WORDS / OVER; ++w) convert(w, std::integral_constant<int, ST + 2>{});
+        }
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      float mx = s_cur[0];
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        pv(0, db);
+        read_k(db);
+        convert_at(db);
+#pragma unroll
+        for (int e = 16 / DB * db; e < 16 / DB * (db + 1); ++e) mx = fmaxf(mx, s_cur[e]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mx = xhalf_max(mx) * sc;
+      const bool need = mx > m_run + 8.0f;
+      if (__any(need)) {
+        // (rare after the first tiles) the accumulator changes its reference; the half of tile t-1's probabilities whose product is still to
+        // come belongs to the old one and is scaled with it
+        const float corr = need ? __builtin_amdgcn_exp2f(m_run - mx) : 1.0f;
+        m_run = need ? mx : m_run;
+        l_run *= corr;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc_o[db][e] *= corr;
+        const uint4 w = __builtin_bit_cast(uint4, pf[1]);
+        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = pack_bf16(__uint_as_float(ww[q] << 16) * corr, __uint_as_float(ww[q] & 0xffff0000u) * corr);
+        pf[1] = __builtin_bit_cast(bf16x8, uint4{o[0], o[1], o[2], o[3]});
+      }
+      const float neg_ref = (m_run == -INFINITY) ? 0.f : -m_run;
+      float pe[16], ps0 = 0.f, ps1 = 0.f;
+      typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+      uintx4 pw[2];
+      const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3f803f80u);
+      floatx16 s_next;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s_next[e] = 0.f;
+      // e4m3: the row sum is taken over the rounded probabilities, the values that P V uses.  int8: the scale of the value joins the
+      // probability ahead of its one rounding, and the sum is over what there was before.
+      auto round_pair = [&](int i) {
+        float &ps = (i & 1) ? ps1 : ps0;
+        uint32_t w;
+        if constexpr (F == Q_E4M3) {
+          w = pack_bf16(pe[2 * i], pe[2 * i + 1]);
+          ps = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), ones, ps, false);
+        } else {
+          const float2 v2 = *reinterpret_cast<const float2 *>(scales + 4 * TK + 32 * (i / 2) + 8 * (i % 2));
+          ps += pe[2 * i] + pe[2 * i + 1];
+          w = pack_bf16(pe[2 * i] * v2.x, pe[2 * i + 1] * v2.y);
+        }
+        pw[i / 4][i % 4] = w;
+      };
+      auto exps = [](int slot) { return slot < 0 ? 0 : 16 * (slot + 1) / SLOTS; };  // taken by then
+#pragma unroll
+      for (int slot = 0; slot < SLOTS; ++slot) {
+        if (slot < DB) {  // (KK is 2 DB)
+          pv(1, slot);
+          read_v(0, slot);
+        } else {
+          s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[(slot - DB) % DB], qf[slot - DB], s_next, 0, 0, 0);
+          if (slot < 2 * DB) {
+            read_k(slot);
+            read_v(1, slot - DB);
+          }
+        }
+        convert_at(DB + slot);
+#pragma unroll
+        for (int e = exps(slot - 1); e < exps(slot); ++e) {
+          pe[e] = __builtin_amdgcn_exp2f(fmaf(s_cur[e], sc, neg_ref));
+          here(pe[e]);
+        }
+#pragma unroll
+        for (int i = exps(slot - 2) / 2; i < exps(slot - 1) / 2; ++i) round_pair(i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = exps(SLOTS - 2) / 2; i < 8; ++i) round_pair(i);
+      if (STEADY || t + 2 + NR < n_tiles) issue(t + 2 + NR, std::integral_constant<int, ST + 2 + NR>{}, steady_c);  // (the codes that lay there have been converted)
+      l_run += ps0 + ps1;  // (this lane's keys; the other half's are added behind the loop)
+      pf[0] = __builtin_bit_cast(bf16x8, pw[0]);
+      pf[1] = __builtin_bit_cast(bf16x8, pw[1]);
+      s_cur = s_next;
+    };
+    {
+      int t = 0;
+      for (; t + T::CYCLE + 2 + NR < n_tiles; t += T::CYCLE) {  // (each with a tile to copy that is not the last)
+        body(t, std::true_type{}, std::integral_constant<int, 0>{});
+        body(t + 1, std::true_type{}, std::integral_constant<int, 1>{});
+        body(t + 2, std::true_type{}, std::integral_constant<int, 2>{});
+        body(t + 3, std::true_type{}, std::integral_constant<int, 3>{});
+        body(t + 4, std::true_type{}, std::integral_constant<int, 4>{});
+        body(t + 5, std::true_type{}, std::integral_constant<int, 5>{});
+      }
+      cycles(t, n_tiles, [&](int u, auto st_c) { body(u, std::false_type{}, st_c); });
     }
-    const float neg_ref = (m_run == -INFINITY) ? 0.f : -m_run;
-    uint32_t pw[8];
-    float ps = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; e += 2) {
-      const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], sc, neg_ref));
-      const float p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], sc, neg_ref));
-      const uint32_t w = pack_bf16(p0, p1);
-      ps += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
-      pw[e >> 1] = w;
-    }
-    l_run += xhalf_sum(ps);
-    const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, uint4{pw[0], pw[1], pw[2], pw[3]}),
-                          __builtin_bit_cast(bf16x8, uint4{pw[4], pw[5], pw[6], pw[7]})};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const int row = vrow + ks * 16;
-        const unsigned char *p = smem + T::REGION + row * ROWB + 8 * (lane % 4) + T::v_pair(row, db * 2 + hb) * 32;
-        const shortx4 g0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p));
-        const shortx4 g1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + 8 * ROWB));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7));
-        acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], acc_o[db], 0, 0, 0);
-      }
+      for (int db = 0; db < DB; ++db) pv(ks, db);  // the last tile's
+    l_run = xhalf_sum(l_run);
   }
-
-  // merge the wave columns of each query block through LDS
-  if constexpr (WK > 1) {
-    float *mg = reinterpret_cast<float *>(smem);
-    __syncthreads();
-    if (wk > 0) {
-      float *dst = mg + (size_t)((wk - 1) * WQ + wq) * T::PER_WAVE + lane;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) dst[(db * 16 + e) * 64] = acc_o[db][e];
-      dst[(DB * 16) * 64] = m_run;
-      dst[(DB * 16 + 1) * 64] = l_run;
-    }
-    __syncthreads();
-    if (wk > 0) return;
-    float M = m_run;
-#pragma unroll
-    for (int w = 1; w < WK; ++w) M = fmaxf(M, mg[(size_t)((w - 1) * WQ + wq) * T::PER_WAVE + (DB * 16) * 64 + lane]);
-    const float Ms = (M == -INFINITY) ? 0.f : M;
-    const float c0 = __builtin_amdgcn_exp2f(m_run - Ms);
-    l_run *= c0;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc_o[db][e] *= c0;
-#pragma unroll
-    for (int w = 1; w < WK; ++w) {
-      const float *src = mg + (size_t)((w - 1) * WQ + wq) * T::PER_WAVE + lane;
-      const float cw = __builtin_amdgcn_exp2f(src[(DB * 16) * 64] - Ms);
-      l_run = fmaf(src[(DB * 16 + 1) * 64], cw, l_run);
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc_o[db][e] = fmaf(src[(db * 16 + e) * 64], cw, acc_o[db][e]);
-    }
-    m_run = M;
-  }
-  if (wq * 32 + l32 >= nq) return;
+  __syncthreads();  // every wave is done with the tiles
+  if (wave * 32 >= nq) return;
   if (a.splits == 1) {
-    const float inv = k_lo < k_hi ? 1.0f / l_run : 0.f;  // (a sequence without keys: zeros)
-    bf16_t *out = (bf16_t *)a.out + ((size_t)jq * a.H + hq) * DH + 4 * lhi;
+    // whole rows leave by way of LDS: 16-byte chunk c of row r lies at c ^ (r % chunks)
+    constexpr int CH = DH / 8, RPI = WAVE / CH;
+    unsigned char *rows = smem + wave * 32 * ROWB;
+    const float inv = n_tiles > 0 ? 1.0f / l_run : 0.f;  // (a sequence without keys: zeros)
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<uint2 *>(out + db * 32 + 8 * g) =
+        *reinterpret_cast<uint2 *>(rows + l32 * ROWB + (((db * 4 + g) ^ (l32 % CH)) * 16) + lhi * 8) =
             uint2{pack_bf16(acc_o[db][4 * g] * inv, acc_o[db][4 * g + 1] * inv), pack_bf16(acc_o[db][4 * g + 2] * inv, acc_o[db][4 * g + 3] * inv)};
-  } else {
-    const size_t at = ((size_t)split * a.rows.cap + jq) * a.H + hq;
-    float *po = a.part_o + at * DH + 4 * lhi;
+    asm volatile("" : : : "memory");  // the reads below are of another type (LDS accesses of a wave keep their order)
+    const uint32_t place = (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq;
+    const int cc = lane % CH;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4 *>(po + db * 32 + 8 * g) = float4{acc_o[db][4 * g], acc_o[db][4 * g + 1], acc_o[db][4 * g + 2], acc_o[db][4 * g + 3]};
-    // a split without a key counts for nothing; where all are without one, the first makes the row zero
-    if (lhi == 0) {
-      const bool none = k_lo >= k_hi;
-      *reinterpret_cast<float2 *>(a.part_ml + at * 2) = float2{none && split == 0 ? 0.f : m_run * LN2, none && split == 0 ? 1.f : l_run};
+    for (int i = 0; i < 32 / RPI; ++i) {
+      const int r = RPI * i + lane / CH;
+      const uint4 v = *reinterpret_cast<const uint4 *>(rows + r * ROWB + ((cc ^ (r % CH)) * 16));
+      const uint32_t at = (uint32_t)__shfl((int)place, r, WAVE);
+      if (wave * 32 + r < nq) *(reinterpret_cast<uint4 *>((bf16_t *)a.out + (size_t)at * DH) + cc) = v;
     }
+    return;
+  }
+  if (wave * 32 + l32 < nq) store_partial<DH>(a, acc_o, split, (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq, lhi, n_tiles == 0, m_run, l_run);
+}
+
+template <int DH, int NW> void launch_tile(const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
+  const int q_tiles = max_q_tiles_grouped(a, 32 * NW), grid = attn_grid_grouped(a, q_tiles);
+  if (q.format == Q_E4M3) k_attn_quant_tile<DH, Q_E4M3, NW><<<grid, 64 * NW, 0, s>>>(a, q, q_tiles);
+  else k_attn_quant_tile<DH, Q_INT8, NW><<<grid, 64 * NW, 0, s>>>(a, q, q_tiles);
+}
+// ---- merge of the splits: a wave to a (row, head), its lanes the splits' weights, then the columns -------------
+constexpr int MAX_SPLITS = 128;
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_quant_merge(AttnArgs a) {
+  constexpr int V = DH / WAVE;
+  const int n = a.rows.count ? min(*a.rows.count, a.rows.cap) : a.rows.cap, lane = threadIdx.x % WAVE;
+  const uint32_t items = (uint32_t)n * (uint32_t)a.H;
+  const size_t step = (size_t)a.rows.cap * a.H;
+  for (uint32_t it = blockIdx.x * 4 + threadIdx.x / WAVE; it < items; it += gridDim.x * 4) {
+    float m[2], l[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int s = lane + u * WAVE;
+      const float2 ml = s < a.splits ? *reinterpret_cast<const float2 *>(a.part_ml + ((size_t)s * step + it) * 2) : float2{-INFINITY, 0.f};
+      m[u] = ml.x; l[u] = ml.y;
+    }
+    // (as in the kernels before: a maximum that is no number leaves the weights so)
+    const float M = wave_max(fmaxf(m[0], m[1])), ref = M == -INFINITY ? 0.f : M;
+    float w[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) w[u] = __expf(m[u] - ref);
+    const float total = wave_sum(l[0] * w[0] + l[1] * w[1]);
+    float o[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = 0.f;
+    const float *po = a.part_o + (size_t)it * DH + lane * V;
+    auto weight = [&](int s) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s < WAVE ? w[0] : w[1]), s % WAVE)); };
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {  // (eight loads in flight; past the end the last split again, with no weight)
+      float x[8][V];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i][e] = po[(size_t)min(s0 + i, a.splits - 1) * step * DH + e];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float ws = s0 + i < a.splits ? weight(s0 + i) : 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = fmaf(x[i][e], ws, o[e]);
+      }
+    }
+    const float inv = 1.0f / total;
+    T *out = (T *)a.out + (size_t)it * DH + lane * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) out[e] = from_f<T>(o[e] * inv);
   }
 }
 
-template <int DH, int WQ, int WK> void launch_tile(const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
-  using T = QTile<DH, WQ, WK>;
-  const int q_tiles = max_q_tiles_grouped(a, T::BQ), grid = attn_grid_grouped(a, q_tiles);
-  if (q.format == Q_E4M3) k_attn_quant<DH, WQ, WK, Q_E4M3><<<grid, T::NT, 0, s>>>(a, q, q_tiles);
-  else k_attn_quant<DH, WQ, WK, Q_INT8><<<grid, T::NT, 0, s>>>(a, q, q_tiles);
+template <typename T> void launch_merge(const AttnArgs &a, hipStream_t s) {
+  const long blocks = ((long)a.rows.cap * a.H + 3) / 4;
+  const int grid = (int)(blocks > 8192 ? 8192 : blocks);
+  if (a.dh == 64) k_quant_merge<T, 64><<<grid, 256, 0, s>>>(a);
+  else k_quant_merge<T, 128><<<grid, 256, 0, s>>>(a);
 }
 
 // fp32 queries and results: 16 rows x 16 lanes a workgroup, tiles of 32 keys; codes become fp32 values on their way into LDS.
@@ -340,21 +885,38 @@ __global__ __launch_bounds__(256) void k_attn_quant_f32(AttnArgs a, QuantAttn qc
 
 }  // namespace
 
-// Query tile (32, 64 or 128 packed rows) and key splits.
+// Query tile and key splits.  The prices are fits to timed launches (heads of 128, e4m3 and int8 within 10 %), ns of a workgroup per key:
+//   32 rows a workgroup   7 while each CU has one; 15.5 for the 512 that the chip holds, and so on in proportion
+//   256 rows              28.5 for the 256 that the chip holds (heads of 64: 128 rows, 25, 512 of them; the 32-row form 5 and 8.5)
+// so 32 rows a workgroup are taken for few rows or few sequences.  32 / 256 rows, us: 285 rows of 16 sequences, 1280 keys at most,
+// 45.6 / 71.3; 1941 rows 105 / 81; 1554 rows of 16 x 2048 keys 125 / 112; 102 rows of one sequence of 1024 13.5 / 24.5; 28 heads over 4,
+// 1137 rows of 13 x 1277 48.3 / 50.3; heads of 64 over 2, 7764 rows of 16 x 2048 78 / 55.
+// Splits pay a second launch and the partial results' way through memory, so only the 32-row form has them, where a few workgroups
+// would read long sequences: 1 row of 32768 keys, 4 heads, 1 / 8 / 32 / 128 splits 183 / 33.6 / 19.5 / 25.2 us; one row in each of 16
+// sequences of 2048, 1 / 4 / 16 22.7 / 18.0 / 23.5; 102 rows of 1024, 32 heads, 1 / 2 13.5 / 16.7.
 void attention_quant_plan(DType t, size_t part_elems, AttnArgs *a) {
-  const int grp = a->H / a->Hkv;
-  const long rows = a->offsets ? ((long)a->rows.cap + a->B - 1) / a->B : a->L, packed = rows * grp;
-  a->bq = t == F32 ? 16 : packed <= 32 ? 32 : packed <= 64 ? 64 : 128;
-  const int BK = t == F32 ? 32 : 128;
-  const long tiles = t == F32 ? ((rows + 15) / 16) * a->B * a->H : ((packed + a->bq - 1) / a->bq) * a->B * a->Hkv;
-  long s = (512 + tiles - 1) / (tiles < 1 ? 1 : tiles);
-  const long by_keys = ((long)a->L + BK - 1) / BK;
-  if (s > by_keys) s = by_keys;
-  if (s > 128) s = 128;
-  const size_t per_split = (size_t)a->rows.cap * a->H * a->dh;
-  if (per_split > 0 && (size_t)s * per_split > part_elems) s = (long)(part_elems / per_split);
-  if (s < 1) s = 1;
-  a->chunk = split_chunk(a->L, (int)s, BK);
+  const long grp = a->H / a->Hkv, rows = a->offsets ? ((long)a->rows.cap + a->B - 1) / a->B : a->L, packed = rows * grp;
+  const double pairs = (double)a->B * a->Hkv, d128 = a->dh == 128;
+  auto tiles = [&](int bq) { return pairs * ((packed + bq - 1) / bq); };
+  auto price = [&](double n) { return n * (d128 ? 15.5 : 8.5) / 512 > (d128 ? 7 : 5) ? n * (d128 ? 15.5 : 8.5) / 512 : (d128 ? 7.0 : 5.0); };
+  const int tall = d128 ? 256 : 128;
+  const double resident = d128 ? 256 : 512, n_tall = tiles(tall);
+  a->bq = t == F32 ? 16 : (d128 ? 28.5 : 25.0) * (n_tall > resident ? n_tall / resident : 1) < price(tiles(32)) ? tall : 32;
+  a->splits = 1;
+  const int BK = t == F32 ? 32 : 128;  // keys that the waves of a workgroup take at a time
+  if (t == F32 || a->bq == 32) {
+    const double n = t == F32 ? (double)a->B * a->H * ((rows + 15) / 16) : tiles(32);
+    const size_t per_split = (size_t)a->rows.cap * a->H * a->dh;
+    double best = 0;
+    for (int s = 1; s <= MAX_SPLITS && (long)(s - 1) * BK < a->L && (s == 1 || s * per_split <= part_elems); ++s) {
+      const double ns = a->L / (double)s * price(n * s) + (s > 1 ? 3500 + 150.0 * s + 8.0 * s * per_split / 4000 : 0);
+      if (s == 1 || ns < best) {
+        best = ns;
+        a->splits = s;
+      }
+    }
+  }
+  a->chunk = split_chunk(a->L, a->splits, BK);
   a->splits = (a->L + a->chunk - 1) / a->chunk;  // drops splits that would be empty
 }
 
@@ -366,16 +928,17 @@ void launch_attention_quant(DType t, const AttnArgs &a, const QuantAttn &q, hipS
     else if (a.dh == 64) k_attn_quant_f32<64, Q_INT8><<<grid, 256, 0, s>>>(a, q);
     else if (q.format == Q_E4M3) k_attn_quant_f32<128, Q_E4M3><<<grid, 256, 0, s>>>(a, q);
     else k_attn_quant_f32<128, Q_INT8><<<grid, 256, 0, s>>>(a, q);
-  } else if (a.dh == 64) {
-    if (a.bq == 32) launch_tile<64, 1, 4>(a, q, s);
-    else if (a.bq == 64) launch_tile<64, 2, 2>(a, q, s);
-    else launch_tile<64, 4, 1>(a, q, s);
-  } else {
-    if (a.bq == 32) launch_tile<128, 1, 4>(a, q, s);
-    else if (a.bq == 64) launch_tile<128, 2, 2>(a, q, s);
-    else launch_tile<128, 4, 1>(a, q, s);
+    if (a.splits > 1) launch_merge<float>(a, s);
+    return;
   }
-  if (a.splits > 1) launch_attn_combine(t, a, s);
+  if (a.bq == 32) {
+    if (a.dh == 64) launch_stream<64>(a, q, s);
+    else launch_stream<128>(a, q, s);
+  } else {
+    if (a.dh == 64) launch_tile<64, 4>(a, q, s);
+    else launch_tile<128, 8>(a, q, s);
+  }
+  if (a.splits > 1) launch_merge<bf16_t>(a, s);
 }
 
 }  // namespace dy

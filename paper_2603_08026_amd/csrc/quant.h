@@ -57,16 +57,14 @@ template <int F> __device__ __forceinline__ void q_values(uint32_t w, float scal
   }
 }
 
-// four codes -> four bf16 values in two words.  e4m3: exact, and reads the exponent of the scale alone (a NaN gives NaN).  int8: one
-// rounding of the product to bf16, 2^-9 of a value, where the codes themselves are 2^-9 of the largest one off.
+// four codes -> four bf16 values in two words, exact.  e4m3: the values, of the scale the exponent alone (a NaN gives NaN).  int8: the
+// codes, whose scales are applied to what is made of them.
 template <int F> __device__ __forceinline__ uint2 q_bf16(uint32_t w, float scale) {
   if constexpr (F == Q_E4M3) {
     return uint2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))};
   } else {
-    float x[4];
-    q_values<F>(w, scale, x);
-    return uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    return uint2{pack_bf16((float)(int8_t)w, (float)(int8_t)(w >> 8)), pack_bf16((float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24))};
   }
 }
 

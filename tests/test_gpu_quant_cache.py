@@ -86,7 +86,7 @@ def _values(codes, scale):
     return _host(codes) * _host(scale).transpose(0, 2, 1)[..., None]
 
 
-def _attend(q, k, v, idx, off, L, kv_len, t, codes):
+def _attend(q, k, v, off, L, kv_len, t):
     """(rows, tolerances) of exact attention rows in 64 bits; q [n, H, dh], k and v [B, L, Hkv, dh]"""
     n, H, dh = q.shape
     Hkv, u = k.shape[2], U[t]
@@ -103,12 +103,11 @@ def _attend(q, k, v, idx, off, L, kv_len, t, codes):
             p = np.exp(s - s.max(-1, keepdims=True))
             p /= p.sum(-1, keepdims=True)
             out[rows, h] = p @ vb
-            # a score is off by its sum's roundings (dh products and sums, the scaling, the difference to the maximum: under
-            # dh + 8 in fp32) and, bf16 with int8 codes, by the key's rounding; a weight by twice that, the exponential (2^-20),
-            # and in bf16 by its own rounding, twice since the sum is over rounded ones; bf16 with int8 codes by the value's
-            key = u if (t == "bf16" and codes == "int8") else 0.0
-            ds = size.max(-1, keepdims=True) * (key + (dh + 8) * U["f32"])
-            w = np.expm1(2 * ds) + 2.0 ** -20 + N * U["f32"] + (2 * u + key if t == "bf16" else 0.0)
+            # (keys and values, or their codes, are exact in bf16.)  A score is off by its sum's roundings (dh products and sums, the
+            # scales, the difference to the maximum: under dh + 8 in fp32); a weight by twice that, the exponential (2^-20), and in
+            # bf16 by its own rounding, twice where the sum is over rounded ones
+            ds = size.max(-1, keepdims=True) * (dh + 8) * U["f32"]
+            w = np.expm1(2 * ds) + 2.0 ** -20 + N * U["f32"] + (2 * u if t == "bf16" else 0.0)
             tol[rows, h] = w * (p @ np.abs(vb)) * 1.05 + u * np.abs(out[rows, h]) + 1e-30
     return out.reshape(n, H * dh), tol.reshape(n, H * dh)
 
@@ -347,7 +346,7 @@ def _check_attend(seed, t, H, Hkv, dh, B, L, counts, codes, kv_len=None, cap=Non
     ctx.partial_attention_quant(q, c, il, B, L, out, ln)
     torch.cuda.synchronize()
     keep = lambda z: np.nan_to_num(z)  # noqa: E731  (padding, which the rows below never read)
-    want, tol = _attend(_host(q)[:n], keep(_values(c.k, c.k_scale)), keep(_values(c.v, c.v_scale)), idx, off, L, kv_len, t, codes)
+    want, tol = _attend(_host(q)[:n], keep(_values(c.k, c.k_scale)), keep(_values(c.v, c.v_scale)), off, L, kv_len, t)
     _within(out[:n], want, tol, "rows")
     assert torch.all(out[n:] == 7.0)
     ctx.close()
@@ -432,7 +431,7 @@ def test_codes_beyond_four_gigabytes(t):
         assert torch.all((bk.float() - z.float()).abs() <= m * (0.5 / 127 + 2.0 ** -8))
     for h in (0, 31):
         k, v = (cd[last, :, h].double().cpu().numpy() * sc[last, h].double().cpu().numpy()[:, None] for cd, sc in ((c.k, c.k_scale), (c.v, c.v_scale)))
-        want, tol = _attend(_host(q)[:, h:h + 1], k[None, :, None], v[None, :, None], None, np.array([0, 2]), L, None, t, "int8")
+        want, tol = _attend(_host(q)[:, h:h + 1], k[None, :, None], v[None, :, None], np.array([0, 2]), L, None, t)
         _within(out.view(2, H, dh)[:, h], want, tol, "head %d" % h)
     ctx.close()
 
