@@ -145,6 +145,15 @@ def _ptr(t: Optional[torch.Tensor]):
     return C.c_void_p(t.data_ptr())
 
 
+def _device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _raw_stream(device: int) -> int:
+    """The current stream of a device."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _stream() -> C.c_void_p:
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
@@ -187,6 +196,7 @@ class QuantCache:
             if t.device != k.device:
                 raise ValueError("the cache's tensors are on different devices")
         self.k, self.v, self.k_scale, self.v_scale, self.format = k, v, k_scale, v_scale, CODES[k.dtype]
+        self.shape, self.device = tuple(k.shape), k.get_device()
         self.c = QuantCacheC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.format)
 
     @staticmethod
@@ -253,6 +263,8 @@ class Context:
         if rc:
             raise DyllmError(rc, self.lib.dyllm_strerror(rc).decode())
         self.h = h
+        self._dtype = torch.float32 if cfg.dtype == F32 else torch.bfloat16
+        self._dq, self._dkv = cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
 
     def close(self):
         if getattr(self, "h", None):
@@ -357,99 +369,111 @@ class Context:
         return int(self.lib.dyllm_step_kind(C.byref(sched), t))
 
     # ---- normalised query and key heads; the cache in 8 bits.  Tensors are checked against the context: type, number of elements, device.
+    # (A call takes the host about as long as a short kernel the GPU, so what it asks of torch is asked once.)
 
-    def _arg(self, t, numel, what, dtype=None):
-        dtype = dtype or (torch.float32 if self.cfg.dtype == F32 else torch.bfloat16)
-        if t.dtype != dtype or t.numel() < numel or not t.is_contiguous():
+    def _arg(self, t, numel, what, dev, dtype=None):
+        dtype = dtype or self._dtype
+        if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
             raise ValueError("%s: a contiguous %s tensor of at least %d elements is wanted" % (what, dtype, numel))
-        if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        if t.get_device() != dev:
             raise ValueError("%s: not on the current device" % what)
         return t.data_ptr()
 
-    def _gain(self, g, what):
-        return None if g is None else self._arg(g, self.cfg.head_dim, what)
+    def _gain(self, g, what, dev):
+        return None if g is None else self._arg(g, self.cfg.head_dim, what, dev)
 
-    def _rows(self, rows, B, L):
+    def _lens(self, kv_len, B, dev):
+        return None if kv_len is None else self._arg(kv_len, B, "kv_len", dev, torch.int32)
+
+    def _rows(self, rows, B, L, dev):
         """(the list's structure or None, rows at most)"""
         if rows is None:
             return None, B * L
         if rows.offsets.numel() < B + 1:
             raise ValueError("rows: %d offsets are wanted" % (B + 1))
-        return C.byref(rows.c()), rows.cap
+        if rows.idx.get_device() != dev or rows.offsets.get_device() != dev:
+            raise ValueError("rows: not on the current device")
+        c = rows.c()
+        return C.byref(c), c.cap
 
-    def _quant(self, cache: QuantCache, B, L):
-        b, l, hkv, dh = cache.k.shape
-        if (hkv, dh) != (self.cfg.n_kv_heads, self.cfg.head_dim) or (b, l) != (B, L):
-            raise ValueError("the 8-bit cache is [%d, %d, %d, %d], the call's [%d, %d, %d, %d]"
-                             % (b, l, hkv, dh, B, L, self.cfg.n_kv_heads, self.cfg.head_dim))
-        if cache.k.device.index != torch.cuda.current_device():
+    def _quant(self, cache: QuantCache, B, L, dev):
+        if cache.shape != (B, L, self.cfg.n_kv_heads, self.cfg.head_dim):
+            raise ValueError("the 8-bit cache is %s, the call's %s"
+                             % (cache.shape, (B, L, self.cfg.n_kv_heads, self.cfg.head_dim)))
+        if cache.device != dev:
             raise ValueError("the 8-bit cache is not on the current device")
         return C.byref(cache.c)
 
-    def _qkv(self, qkv, n):
+    def _qkv(self, qkv, n, dev):
         """(pointer, row stride) of raw projections [n, (H + 2 Hkv) dh], whose rows may lie further apart than they are long"""
         width = (self.cfg.n_heads + 2 * self.cfg.n_kv_heads) * self.cfg.head_dim
         if qkv.dim() != 2 or qkv.shape[1] != width or qkv.shape[0] < n or qkv.stride(1) != 1 or (n > 1 and qkv.stride(0) < width):
             raise ValueError("qkv: [%d, %d] with neighbouring columns is wanted" % (n, width))
-        ld = qkv.stride(0) if qkv.shape[0] > 1 else width
-        if qkv.dtype != (torch.float32 if self.cfg.dtype == F32 else torch.bfloat16) or qkv.device.index != torch.cuda.current_device():
+        if qkv.dtype is not self._dtype or qkv.get_device() != dev:
             raise ValueError("qkv: of another type or device than the context's")
-        return qkv.data_ptr(), ld
+        return qkv.data_ptr(), qkv.stride(0) if qkv.shape[0] > 1 else width
 
     def head_norm_rope(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: LayerCache, q_out):
         """qkv: [n, (H + 2 Hkv) dh], rows may be strided; g_q, g_k: [dh] or None; rows None: all B*L tokens."""
-        r, n = self._rows(rows, B, L)
-        p, ld = self._qkv(qkv, n)
-        q = self._arg(q_out, n * self.cfg.n_heads * self.cfg.head_dim, "q_out")
-        self._check(self.lib.dyllm_head_norm_rope(self.h, p, ld, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), r, B, L,
-                                                  C.byref(cache), q, _stream()))
+        dev = _device()
+        r, n = self._rows(rows, B, L, dev)
+        p, ld = self._qkv(qkv, n, dev)
+        q = self._arg(q_out, n * self._dq, "q_out", dev)
+        self._check(self.lib.dyllm_head_norm_rope(self.h, p, ld, self._gain(g_q, "g_q", dev), self._gain(g_k, "g_k", dev), r, B,
+                                                  L, C.byref(cache), q, _raw_stream(dev)))
 
     def head_norm_rope_quant(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: QuantCache, q_out):
-        r, n = self._rows(rows, B, L)
-        p, ld = self._qkv(qkv, n)
-        q = self._arg(q_out, n * self.cfg.n_heads * self.cfg.head_dim, "q_out")
-        self._check(self.lib.dyllm_head_norm_rope_quant(self.h, p, ld, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), r, B,
-                                                        L, self._quant(cache, B, L), q, _stream()))
+        dev = _device()
+        r, n = self._rows(rows, B, L, dev)
+        p, ld = self._qkv(qkv, n, dev)
+        q = self._arg(q_out, n * self._dq, "q_out", dev)
+        self._check(self.lib.dyllm_head_norm_rope_quant(self.h, p, ld, self._gain(g_q, "g_q", dev), self._gain(g_k, "g_k", dev), r,
+                                                        B, L, self._quant(cache, B, L, dev), q, _raw_stream(dev)))
 
     def quant_write(self, k, v, rows: Optional[IndexList], B, L, cache: QuantCache):
-        r, n = self._rows(rows, B, L)
-        n *= self.cfg.n_kv_heads * self.cfg.head_dim
-        self._check(self.lib.dyllm_quant_write(self.h, self._arg(k, n, "k"), self._arg(v, n, "v"), r, B, L,
-                                               self._quant(cache, B, L), _stream()))
+        dev = _device()
+        r, n = self._rows(rows, B, L, dev)
+        n *= self._dkv
+        self._check(self.lib.dyllm_quant_write(self.h, self._arg(k, n, "k", dev), self._arg(v, n, "v", dev), r, B, L,
+                                               self._quant(cache, B, L, dev), _raw_stream(dev)))
 
     def quant_read(self, cache: QuantCache, rows: Optional[IndexList], B, L, k_out, v_out):
-        r, n = self._rows(rows, B, L)
-        n *= self.cfg.n_kv_heads * self.cfg.head_dim
-        self._check(self.lib.dyllm_quant_read(self.h, self._quant(cache, B, L), r, B, L, self._arg(k_out, n, "k_out"),
-                                              self._arg(v_out, n, "v_out"), _stream()))
+        dev = _device()
+        r, n = self._rows(rows, B, L, dev)
+        n *= self._dkv
+        self._check(self.lib.dyllm_quant_read(self.h, self._quant(cache, B, L, dev), r, B, L, self._arg(k_out, n, "k_out", dev),
+                                              self._arg(v_out, n, "v_out", dev), _raw_stream(dev)))
 
     def partial_attention_quant(self, q_sal, cache: QuantCache, rows: Optional[IndexList], B, L, c_sal_out, kv_len=None):
         """kv_len: int32 [B] device tensor (keys of each sequence) or None."""
-        r, n = self._rows(rows, B, L)
-        n *= self.cfg.n_heads * self.cfg.head_dim
+        dev = _device()
+        r, n = self._rows(rows, B, L, dev)
+        n *= self._dq
         self._check(self.lib.dyllm_partial_attention_quant(
-            self.h, self._arg(q_sal, n, "q_sal"), self._quant(cache, B, L),
-            None if kv_len is None else self._arg(kv_len, B, "kv_len", torch.int32), r, B, L,
-            self._arg(c_sal_out, n, "c_sal_out"), _stream()))
+            self.h, self._arg(q_sal, n, "q_sal", dev), self._quant(cache, B, L, dev), self._lens(kv_len, B, dev), r, B, L,
+            self._arg(c_sal_out, n, "c_sal_out", dev), _raw_stream(dev)))
 
     def qkv_refresh_normed(self, w: LayerWeights, g_q, g_k, x, rows: Optional[IndexList], B, L, cache, q_sal_out):
         """cache: LayerCache (storage type) or QuantCache."""
-        r, n = self._rows(rows, B, L)
+        dev = _device()
+        r, n = self._rows(rows, B, L, dev)
         quant = isinstance(cache, QuantCache)
         self._check(self.lib.dyllm_qkv_refresh_normed(
-            self.h, C.byref(w), self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), self._arg(x, B * L * self.cfg.hidden, "x"), r,
-            B, L, None if quant else C.byref(cache), self._quant(cache, B, L) if quant else None,
-            self._arg(q_sal_out, n * self.cfg.n_heads * self.cfg.head_dim, "q_sal_out"), _stream()))
+            self.h, C.byref(w), self._gain(g_q, "g_q", dev), self._gain(g_k, "g_k", dev),
+            self._arg(x, B * L * self.cfg.hidden, "x", dev), r, B, L, None if quant else C.byref(cache),
+            self._quant(cache, B, L, dev) if quant else None, self._arg(q_sal_out, n * self._dq, "q_sal_out", dev),
+            _raw_stream(dev)))
 
     def layer_step_quant(self, w: LayerWeights, g_q, g_k, cache: LayerCache, quant: QuantCache, x, idx_in: IndexList, B, L,
                          tau, idx_out: IndexList, cos_out=None, kv_len=None):
         """Of cache only c and out are used."""
-        i, o = self._rows(idx_in, B, L)[0], idx_out.c()
+        dev = _device()
+        i, n = self._rows(idx_in, B, L, dev)
+        o, _ = self._rows(idx_out, B, L, dev)
         self._check(self.lib.dyllm_layer_step_quant(
-            self.h, C.byref(w), self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), C.byref(cache), self._quant(quant, B, L),
-            None if kv_len is None else self._arg(kv_len, B, "kv_len", torch.int32),
-            self._arg(x, B * L * self.cfg.hidden, "x"), i, B, L, tau, C.byref(o),
-            None if cos_out is None else self._arg(cos_out, idx_in.cap, "cos_out", torch.float32), _stream()))
+            self.h, C.byref(w), self._gain(g_q, "g_q", dev), self._gain(g_k, "g_k", dev), C.byref(cache),
+            self._quant(quant, B, L, dev), self._lens(kv_len, B, dev), self._arg(x, B * L * self.cfg.hidden, "x", dev), i, B, L,
+            tau, o, None if cos_out is None else self._arg(cos_out, n, "cos_out", dev, torch.float32), _raw_stream(dev)))
 
     def full_step(self, w: LayerWeights, cache: LayerCache, x, B, L):
         self._check(self.lib.dyllm_full_step(self.h, C.byref(w), C.byref(cache), _ptr(x), B, L, _stream()))

@@ -386,6 +386,26 @@ def test_attention_of_flat_and_of_sharp_rows(q_size):
     _check_attend(56, "bf16", 4, 4, 128, 2, 900, (20, 130), "e4m3", q_size=q_size)
 
 
+# Many rows take workgroups of 256 rows (heads of 64: 128), where these outnumber the chip's places in the 32-row form: all rows of many
+# sequences, lengths around a tile's and around the turns of its rings, rows that leave waves idle and end inside one
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("dh,B", [(128, 64), (64, 104)])
+@pytest.mark.parametrize("L", [16, 33, 64, 65, 97, 160, 193, 225, 260])
+def test_attention_of_all_rows(dh, B, L, codes):
+    _check_attend(58, "bf16", 32, 1, dh, B, L, (L,) * B, codes)
+
+
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("dh,Hkv", [(128, 2), (64, 4)])
+def test_attention_of_many_ragged_rows(dh, Hkv, codes):
+    """28 heads over 2 or 4, rows of 1 to all of a sequence's tokens, lengths from no key to all."""
+    B, L = 32, 300
+    g = W.philox(59)
+    counts = [300, 1, 0, 290, 19, 55, 73, 128] + [int(n) for n in g.integers(200, 301, B - 8)]
+    kv_len = [300, 300, 300, 0, 1, 31, 32, 33, 64, 95, 96, 97] + [int(n) for n in g.integers(0, 301, B - 12)]
+    _check_attend(59, "bf16", 28, Hkv, dh, B, L, counts, codes, kv_len=kv_len, cap=sum(counts) + 40)
+
+
 def test_attention_of_all_tokens_is_the_full_list():
     t, H, Hkv, dh, B, L = "bf16", 4, 2, 128, 2, 200
     _say("attention: rows None")
