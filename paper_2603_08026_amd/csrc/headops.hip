@@ -65,6 +65,7 @@ __global__ __launch_bounds__(HB) void k_heads(HeadsArgs a) {
   if (SUMS && sp.dev) { sp.n = a.splits.dev[0]; sp.tail_from = a.splits.dev[1]; sp.n_tail = a.splits.dev[2]; }
   const int lane = threadIdx.x % WAVE, sub = lane % LPH;
   const int HT = a.H + 2 * a.Hkv, groups = (HT + HPW - 1) / HPW;
+  // a wave to a row's vectors of one group; neighbouring waves take neighbouring groups
   const uint32_t items = (uint32_t)n * (uint32_t)groups;
   for (uint32_t it = blockIdx.x * WPB + threadIdx.x / WAVE; it < items; it += gridDim.x * WPB) {
     const int j = (int)(it / (uint32_t)groups), head = (int)(it % (uint32_t)groups) * HPW + lane / LPH;
@@ -142,34 +143,34 @@ __global__ __launch_bounds__(HB) void k_heads(HeadsArgs a) {
   }
 }
 
-// a lane takes 16 neighbouring codes
-template <typename T, int F>
-__global__ __launch_bounds__(HB) void k_quant_read(QuantCache c, Rows rows, int L, int Hkv, int dh, T *k_out, T *v_out) {
+// a lane takes 8 neighbouring codes, dh / 8 lanes a vector
+template <typename T, int F, int DH>
+__global__ __launch_bounds__(HB) void k_quant_read(QuantCache c, Rows rows, int L, int Hkv, T *k_out, T *v_out) {
+  constexpr int LPH = DH / 8, HPW = WAVE / LPH;
   const int n = rows.count ? min(*rows.count, rows.cap) : rows.cap;
-  const uint32_t lph = dh / 16, per_row = 2u * Hkv * lph;
-  const uint64_t items = (uint64_t)n * per_row;
-  for (uint64_t it = (uint64_t)blockIdx.x * HB + threadIdx.x; it < items; it += (uint64_t)gridDim.x * HB) {
-    const int j = (int)(it / per_row);
-    const uint32_t in = (uint32_t)(it % per_row), sub = in % lph;
-    const bool isv = in / lph >= (uint32_t)Hkv;
-    const int h = (int)(in / lph) - (isv ? Hkv : 0);
+  const int lane = threadIdx.x % WAVE, sub = lane % LPH;
+  const int groups = (2 * Hkv + HPW - 1) / HPW;
+  const uint32_t items = (uint32_t)n * (uint32_t)groups;
+  for (uint32_t it = blockIdx.x * WPB + threadIdx.x / WAVE; it < items; it += gridDim.x * WPB) {
+    const int j = (int)(it / (uint32_t)groups), vec = (int)(it % (uint32_t)groups) * HPW + lane / LPH;
+    if (vec >= 2 * Hkv) continue;
+    const bool isv = vec >= Hkv;
+    const int h = isv ? vec - Hkv : vec;
     const int r = rows.idx ? rows.idx[j] : j;
-    const uint4 w = *reinterpret_cast<const uint4 *>((isv ? c.v : c.k) + ((size_t)r * Hkv + h) * dh + 16 * sub);
+    const uint2 w = *reinterpret_cast<const uint2 *>((isv ? c.v : c.k) + ((size_t)r * Hkv + h) * DH + 8 * sub);
     const float scale = (isv ? c.vs : c.ks)[((size_t)(r / L) * Hkv + h) * L + r % L];
-    float x[16];
+    float x[8];
     q_values<F>(w.x, scale, x);
     q_values<F>(w.y, scale, x + 4);
-    q_values<F>(w.z, scale, x + 8);
-    q_values<F>(w.w, scale, x + 12);
-    T *dst = (isv ? v_out : k_out) + ((size_t)j * Hkv + h) * dh + 16 * sub;
-    store8(dst, x);
-    store8(dst + 8, x + 8);
+    store8((isv ? v_out : k_out) + ((size_t)j * Hkv + h) * DH + 8 * sub, x);
   }
 }
 
-// (a list's capacity may be far above its count, which the device knows: workgroups without a row are not free)
+// A list's capacity may be far above its count, which the device knows, and workgroups without a row are not free; with fewer of them the
+// others take their rows in turn, which costs more: 20480 listed rows of 12288 columns, 2048 / 4096 / 8192 / 16384 / 65536 workgroups
+// 207 / 191 / 187 / 179 / 174 us.
 inline int grid_of(uint64_t blocks, const Rows &rows) {
-  const uint64_t most = rows.count ? 4096 : 1 << 20;
+  const uint64_t most = rows.count ? 16384 : 1 << 20;
   return (int)(blocks < 1 ? 1 : blocks > most ? most : blocks);
 }
 
@@ -201,11 +202,17 @@ void launch_heads(DType t, const HeadsArgs &a, bool sums, int dh, int to, hipStr
 
 void launch_quant_read(DType t, const QuantCache &c, int format, Rows rows, int L, int Hkv, int dh, void *k_out, void *v_out, hipStream_t s) {
   if (rows.cap <= 0) return;
-  const int grid = grid_of(((uint64_t)rows.cap * 2 * Hkv * (dh / 16) + HB - 1) / HB, rows);
-  auto go = [&](auto zero) {
+  const int hpw = WAVE / (dh / 8), groups = (2 * Hkv + hpw - 1) / hpw;
+  const int grid = grid_of(((uint64_t)rows.cap * groups + WPB - 1) / WPB, rows);
+  auto with = [&](auto zero, auto dh_c) {
     using T = decltype(zero);
-    if (format == Q_E4M3) k_quant_read<T, Q_E4M3><<<grid, HB, 0, s>>>(c, rows, L, Hkv, dh, (T *)k_out, (T *)v_out);
-    else k_quant_read<T, Q_INT8><<<grid, HB, 0, s>>>(c, rows, L, Hkv, dh, (T *)k_out, (T *)v_out);
+    constexpr int D = decltype(dh_c)::value;
+    if (format == Q_E4M3) k_quant_read<T, Q_E4M3, D><<<grid, HB, 0, s>>>(c, rows, L, Hkv, (T *)k_out, (T *)v_out);
+    else k_quant_read<T, Q_INT8, D><<<grid, HB, 0, s>>>(c, rows, L, Hkv, (T *)k_out, (T *)v_out);
+  };
+  auto go = [&](auto zero) {
+    if (dh == 64) with(zero, std::integral_constant<int, 64>{});
+    else with(zero, std::integral_constant<int, 128>{});
   };
   if (t == F32) go(float{});
   else go(bf16_t{});
