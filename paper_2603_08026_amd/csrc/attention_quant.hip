@@ -46,6 +46,16 @@ __device__ __forceinline__ void store_partial(const AttnArgs &a, const floatx16 
   if (lhi == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = float2{none && split == 0 ? 0.f : m_run * LN2, none && split == 0 ? 1.f : l_run};
 }
 
+// ---- 32 packed query rows a workgroup: few rows ------------------------------------------------------------
+// Bound by the codes' way from memory (one row of 8 x 32768 keys: 401 us for 2.2 GB, 5.5 TB/s) and, where several workgroups read the same
+// keys, by the conversion of every code to bf16, which each repeats.  So the four waves share nothing: each streams key tiles of its own
+// (tile wave, wave + 4, ..) through its own ring in LDS, with no barrier in the loop, and their results are merged once at the end.  Products
+// are S^T = K Q^T and O^T = V^T P^T: a lane's scores are those of one query, so that maximum and sum need one exchange between the
+// halves of the wave, and P has the layout that the second product wants.  K: a lane reads 16 codes at a time and converts them where they
+// are.  V: the transposing 8-bit read gives a lane one column of eight keys.  A key's V scale is the same for all columns and joins the
+// probability in fp32 ahead of its one rounding; its K scale, a power of two, joins the conversion (int8: the score).
+// Two stages a wave leave room for two workgroups a CU, which hide each other's latencies: 285 rows of 16 sequences of 1280 keys at most,
+// int8, 43 us; four stages and one workgroup a CU 57.
 template <int DH_> struct STile {
   static constexpr int DH = DH_, NW = 4, NS = 2;
   static constexpr int BQ = 32, TK = 32;                        // query rows, keys of a wave's tile
@@ -354,32 +364,38 @@ template <int DH> void launch_stream(const AttnArgs &a, const QuantAttn &q, hipS
   else k_attn_quant_stream<DH, Q_INT8><<<grid, 256, 0, s>>>(a, q, q_tiles);
 }
 
-// ---- 128 query rows a workgroup ------------------------------------------------------------------------
-template <int DH_, int NW_> struct QTile {
-  static constexpr int DH = DH_, NW = NW_, NT = 64 * NW, BQ = 32 * NW, TK = 32;
+// ---- 256 packed query rows a workgroup (heads of 64: 128): many rows -------------------------------------------
+// Bound by instruction issue: a 32-key tile costs a SIMD 1024 cycles of matrix instructions and takes 1900, the rest being exponentials,
+// the maximum, LDS reads and the barrier.  A code is converted to bf16 once for all rows of the workgroup: each lane copies 16 codes of a
+// tile straight into LDS, several tiles ahead, converts them two tiles ahead of their use and writes them to a ring of bf16 tiles that every
+// wave reads, V by the transposing read.  A wave waits for its own copies alone, since it converts what it has copied; one barrier a tile.
+// While the vector ALU takes the exponentials of tile t and converts tile t + 2, the matrix pipe works through P V of tile t - 1 and the
+// scores of tile t + 1.  The running reference of the softmax moves only where the maximum exceeds it by 2^8, which is rare.
+// All rings repeat after six tiles and the loop is unrolled by that, so that LDS addresses are constants: 5 % (345 -> 326 us for 7766 rows
+// of 16 x 2048 keys, 32 heads).  Other shapes tried there: 128 rows, four waves, two workgroups a CU 317 us to 312; 64 rows a wave, keys of
+// its own, 373; 64 rows a wave and shared conversion 457; a barrier every second tile 330.
+template <int DH_> struct QTile {
+  static constexpr int DH = DH_, NW = DH == 128 ? 8 : 4, NT = 64 * NW, BQ = 32 * NW, TK = 32;
   static constexpr int ROWB = DH * 2, ROWK = ROWB + 16;             // bytes of a converted row; of K with a gap, so that a lane's reads differ by constants
   static constexpr int HOT_K = TK * ROWK, HOT = TK * ROWB;
   static constexpr int NK = 2, NV = 3, NR = NW == 8 ? 6 : 3, CYCLE = 6;  // converted K and V, tiles of codes and their scales; all repeat after CYCLE
-  static constexpr int RAW = 2 * TK * DH;                           // a tile of codes: K and V, in the order of the lanes that copy them
-  static constexpr int PER = 2 * TK * DH / (NT * 16);               // 16-byte chunks of codes, a lane's share of a tile
+  static constexpr int RAW = 2 * TK * DH;                           // a tile of codes: K and V, in the order of the lanes that copy them, 16 codes a lane
   static constexpr int AT_K = 0, AT_V = NK * HOT_K, AT_RAW = AT_V + NV * HOT, AT_RS = AT_RAW + NR * RAW, AT_SC = AT_RS + NR * NW * 256, LDS = AT_SC + NV * 8 * TK;
   static constexpr int DB = DH / 32, KK = DH / 16, SLOTS = DB + KK;
-  static constexpr int WORDS = 4 * PER;                             // of codes, a lane's share of a tile
-  static_assert(PER >= 1 && PER * NT * 16 == 2 * TK * DH && LDS <= (NW == 8 ? 160 : 80) * 1024 && BQ * ROWB <= LDS,
-                "eight waves to a CU; the rows leave by way of the same memory");
+  static_assert(NT * 16 == RAW && LDS <= (NW == 8 ? 160 : 80) * 1024 && BQ * ROWB <= LDS, "eight waves to a CU; the rows leave by way of the same memory");
   // 32-byte pair p of value row r: the rows that a read serves at a time cover all banks once
   __device__ static __forceinline__ int v_pair(int r, int p) { return DH == 128 ? p ^ (2 * (r & 3)) : p ^ (2 * ((r >> 1) & 1)); }
 };
 
-template <int DH, int F, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, QuantAttn qc, int q_tiles) {
-  using T = QTile<DH, NW>;
-  constexpr int TK = T::TK, ROWB = T::ROWB, DB = T::DB, KK = T::KK, PER = T::PER, SLOTS = T::SLOTS, WORDS = T::WORDS;
+template <int DH, int F>
+__global__ __launch_bounds__(QTile<DH>::NT, 2) void k_attn_quant_tile(AttnArgs a, QuantAttn qc, int q_tiles) {
+  using T = QTile<DH>;
+  constexpr int TK = T::TK, ROWB = T::ROWB, DB = T::DB, KK = T::KK, SLOTS = T::SLOTS, NW = T::NW;
   __shared__ __align__(1024) unsigned char smem[T::LDS];
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int l32 = lane % 32, lhi = lane / 32;
   const AttnItem item = attn_work_item_grouped(a, T::BQ, q_tiles, blockIdx.x);
-  const int b = item.seq, kvh = item.kv_head, split = item.split;
+  const int b = item.seq, kvh = item.kv_head;
   if (b < 0) return;  // uniform: no such tile
   const int nq = item.n, grp = a.H / a.Hkv;
   int jq, hq;  // this lane's query (rows past the end: the last one again, their results are never stored)
@@ -388,9 +404,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
     jq = item.row + p / grp;
     hq = kvh * grp + p % grp;
   }
-  const int Lk = keys_of(qc, a.L, b);
-  const int k_lo = min(split * a.chunk, Lk), k_hi = min(Lk, k_lo + a.chunk);
-  const int n_tiles = (k_hi - k_lo + TK - 1) / TK;
+  const int Lk = keys_of(qc, a.L, b), n_tiles = (Lk + TK - 1) / TK;
 
   bf16x8 qf[KK];
   {
@@ -406,19 +420,15 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
   float m_run = -INFINITY, l_run = 0.f;
   const float sc = LOG2E / sqrtf((float)DH);  // scores are kept in the log2 domain
 
-  // Copies: a wave copies the codes of 8 keys of a tile and their scales, lane by lane where the same lane reads them, so that its own wait
-  // is enough.  A lane's chunk: key own_key, codes 16 own_c and on, of K or of V.  (The halves of an odd key's V change places:
-  // neighbouring keys then write to other banks.)
+  // Copies: a wave copies 16 codes of K or of V a lane (own_v: key own_key of a tile, codes 16 own_c and on) and those keys' scales, all
+  // where the same wave reads them, so that its own wait is enough.  (Heads of 128: half of the waves K, the others V; of 64: half of the lanes.)
   const uint32_t lds0 = lds_offset_of(smem);
   const size_t stride = (size_t)a.Hkv * DH;
   const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH, first_s = ((size_t)b * a.Hkv + kvh) * a.L;
-  auto own_v = [&](int u) { return PER == 2 ? u : DH == 128 ? wave / (NW / 2) : lane / 32; };
-  const int own_8 = DH == 128 && PER == 1 ? wave % (NW / 2) : wave;  // the keys 8 own_8 .. of a tile
-  const int own_key = own_8 * 8 + (DH == 128 ? lane / 8 : (lane % 32) / 4), own_c = DH == 128 ? lane % 8 : lane % 4;
-  const uint8_t *kc = (const uint8_t *)uniform(qc.cache.k + first), *vc = (const uint8_t *)uniform(qc.cache.v + first);
-  const uint8_t *code_at[PER];
-#pragma unroll
-  for (int u = 0; u < PER; ++u) code_at[u] = DH == 128 ? (const uint8_t *)uniform((own_v(u) ? qc.cache.v : qc.cache.k) + first) : nullptr;
+  const int own_v = DH == 128 ? wave / (NW / 2) : lhi, own_8 = DH == 128 ? wave % (NW / 2) : wave;
+  const int own_key = own_8 * 8 + (DH == 128 ? lane / 8 : l32 / 4), own_c = DH == 128 ? lane % 8 : lane % 4;
+  const uint8_t *codes = (own_v ? qc.cache.v : qc.cache.k) + first;
+  if constexpr (DH == 128) codes = (const uint8_t *)uniform(codes);
   const float *src_s = (lane & 8 ? qc.cache.vs : qc.cache.ks) + first_s;  // (8 scales of K, 8 of V, the same again)
   const int scale_key = own_8 * 8 + lane % 8;
   const uint32_t off_full = (uint32_t)own_key * (uint32_t)stride + own_c * 16u;
@@ -426,52 +436,41 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
   auto issue = [&](int t, auto st_c, auto full_c) {
     constexpr int ST = decltype(st_c)::value;
     constexpr bool FULL = decltype(full_c)::value;
-    const uint32_t base = lds0 + T::AT_RAW + (ST % T::NR) * T::RAW + (uint32_t)wave * (PER * 1024u);
-    const int k0 = k_lo + t * TK, last = k_hi - 1 - k0;
+    const uint32_t base = lds0 + T::AT_RAW + (ST % T::NR) * T::RAW + (uint32_t)wave * 1024u;
+    const int k0 = t * TK, last = Lk - 1 - k0;
     const uint32_t off = FULL ? off_full : (uint32_t)min(own_key, last) * (uint32_t)stride + own_c * 16u;
-    if constexpr (DH == 128) {
-#pragma unroll
-      for (int u = 0; u < PER; ++u) dma16_s(code_at[u] + (size_t)k0 * stride, off, base + u * 1024u);
-    } else {
-      dma16((lhi ? vc : kc) + (size_t)k0 * stride + off, base);
-    }
+    if constexpr (DH == 128) dma16_s(codes + (size_t)k0 * stride, off, base);
+    else dma16(codes + (size_t)k0 * stride + off, base);
     dma4(src_s + k0 + (FULL ? scale_key : min(scale_key, last)), lds0 + T::AT_RS + (ST % T::NR) * (NW * 256u) + wave * 256u);
   };
-  auto wait_tiles = [&](auto left_c) { wait_vmcnt<decltype(left_c)::value * (PER + 1)>(); };  // all but the youngest tiles have landed
+  auto wait_tiles = [&](auto left_c) { wait_vmcnt<decltype(left_c)::value * 2>(); };  // all but the youngest tiles have landed
   auto hot_k = [&](int st) { return smem + T::AT_K + (st % T::NK) * T::HOT_K; };
   auto hot_v = [&](int st) { return smem + T::AT_V + (st % T::NV) * T::HOT; };
-  // Conversion: this lane's chunks of a tile, a word of four codes at a time; every second word ends 16 bytes of bf16.
-  uint4 raw[PER];
-  float rs[PER];
+  // Conversion: this lane's codes of a tile, a word of four at a time; every second word ends 16 bytes of bf16.
+  uint4 raw;
+  float rs;
   auto read_raw = [&](auto st_c) {
     constexpr int ST = decltype(st_c)::value;
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      raw[u] = *reinterpret_cast<const uint4 *>(smem + T::AT_RAW + (ST % T::NR) * T::RAW + wave * (PER * 1024) + u * 1024 + lane * 16);
-      rs[u] = *reinterpret_cast<const float *>(smem + T::AT_RS + (ST % T::NR) * (NW * 256) + wave * 256 + own_v(u) * 32 + (own_key % 8) * 4);
-    }
+    raw = *reinterpret_cast<const uint4 *>(smem + T::AT_RAW + (ST % T::NR) * T::RAW + wave * 1024 + lane * 16);
+    rs = *reinterpret_cast<const float *>(smem + T::AT_RS + (ST % T::NR) * (NW * 256) + wave * 256 + own_v * 32 + (own_key % 8) * 4);
   };
-  int own_at[PER];
-#pragma unroll
-  for (int u = 0; u < PER; ++u) own_at[u] = own_v(u) ? own_key * ROWB + T::v_pair(own_key, own_c) * 32 : own_key * T::ROWK + own_c * 32;
+  const int own_at = own_v ? own_key * ROWB + T::v_pair(own_key, own_c) * 32 : own_key * T::ROWK + own_c * 32;
   uint2 even{};
-  auto convert = [&](int w, auto st_c) {
+  auto convert = [&](int i, auto st_c) {
     constexpr int ST = decltype(st_c)::value;
-    const int u = w / 4, i = w % 4, v = own_v(u);
-    const uint32_t word = i == 0 ? raw[u].x : i == 1 ? raw[u].y : i == 2 ? raw[u].z : raw[u].w;
-    const uint2 r = q_bf16<F>(word, rs[u]);
+    const uint2 r = q_bf16<F>(i == 0 ? raw.x : i == 1 ? raw.y : i == 2 ? raw.z : raw.w, rs);
     if (i % 2 == 0) {
       even = r;
     } else {
-      const int stage = v ? T::AT_V + (ST % T::NV) * T::HOT : T::AT_K + (ST % T::NK) * T::HOT_K;
-      *reinterpret_cast<uint4 *>(smem + stage + own_at[u] + i / 2 * 16) = uint4{even.x, even.y, r.x, r.y};
-      if (F == Q_INT8 && i == 3) *reinterpret_cast<float *>(smem + T::AT_SC + (ST % T::NV) * (8 * TK) + v * 4 * TK + own_key * 4) = rs[u];
+      const int stage = own_v ? T::AT_V + (ST % T::NV) * T::HOT : T::AT_K + (ST % T::NK) * T::HOT_K;
+      *reinterpret_cast<uint4 *>(smem + stage + own_at + i / 2 * 16) = uint4{even.x, even.y, r.x, r.y};
+      if (F == Q_INT8 && i == 3) *reinterpret_cast<float *>(smem + T::AT_SC + (ST % T::NV) * (8 * TK) + own_v * 4 * TK + own_key * 4) = rs;
     }
   };
   auto convert_all = [&](auto st_c) {
     read_raw(st_c);
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w) convert(w, st_c);
+    for (int w = 0; w < 4; ++w) convert(w, st_c);
   };
   auto barrier = []() {  // (copies that are under way stay so; the wait is one that the compiler knows of)
     asm volatile("" : : : "memory");
@@ -530,8 +529,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
       if (t + 2 + NR < n_tiles) issue(t + 2 + NR, std::integral_constant<int, ST + 2 + NR>{}, part{});
     });
   } else if (n_tiles > 0) {
-    // While the vector ALU takes the exponentials of tile t and converts tile t + 2, the matrix pipe works through P V of tile t - 1 and
-    // the scores of tile t + 1.
     floatx16 s_cur;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s_cur[e] = 0.f;
@@ -568,7 +565,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
         const shortx4 g1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(p + 8 * ROWB));
         vf[ks][db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7));
       };
-      const int k0 = k_lo + t * TK;
+      const int k0 = t * TK;
       const unsigned char *scales = smem + T::AT_SC + (ST % T::NV) * (8 * TK) + 16 * lhi;  // (int8)
       if constexpr (F == Q_INT8) {
 #pragma unroll
@@ -577,16 +574,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
           s_cur[4 * g] *= k4.x; s_cur[4 * g + 1] *= k4.y; s_cur[4 * g + 2] *= k4.z; s_cur[4 * g + 3] *= k4.w;
         }
       }
-      if (!STEADY && k0 + TK > k_hi) {  // uniform: only the last tile can hold keys past the end
+      if (!STEADY && k0 + TK > Lk) {  // uniform: only the last tile can hold keys past the end
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (k0 + 4 * lhi + 8 * (e / 4) + (e % 4) >= k_hi) s_cur[e] = -INFINITY;
+          if (k0 + 4 * lhi + 8 * (e / 4) + (e % 4) >= Lk) s_cur[e] = -INFINITY;
       }
-      auto convert_at = [&](int product) {  // behind the first twelve of sixteen products, so that all is written well ahead of the barrier
+      auto convert_at = [&](int product) {  // behind the first three quarters of the products, so that all is written well ahead of the barrier
         constexpr int OVER = 3 * DB;
         if (more && product < OVER) {
 #pragma unroll
-          for (int w = product * WORDS / OVER; w < (product + 1) * WORDS / OVER; ++w) convert(w, std::integral_constant<int, ST + 2>{});
+          for (int w = product * 4 / OVER; w < (product + 1) * 4 / OVER; ++w) convert(w, std::integral_constant<int, ST + 2>{});
         }
       };
       __builtin_amdgcn_sched_barrier(0);
@@ -693,38 +690,37 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_quant_tile(AttnArgs a, Quan
   }
   __syncthreads();  // every wave is done with the tiles
   if (wave * 32 >= nq) return;
-  if (a.splits == 1) {
-    // whole rows leave by way of LDS: 16-byte chunk c of row r lies at c ^ (r % chunks)
-    constexpr int CH = DH / 8, RPI = WAVE / CH;
-    unsigned char *rows = smem + wave * 32 * ROWB;
-    const float inv = n_tiles > 0 ? 1.0f / l_run : 0.f;  // (a sequence without keys: zeros)
+  // whole rows leave by way of LDS: 16-byte chunk c of row r lies at c ^ (r % chunks)
+  constexpr int CH = DH / 8, RPI = WAVE / CH;
+  unsigned char *rows = smem + wave * 32 * ROWB;
+  const float inv = n_tiles > 0 ? 1.0f / l_run : 0.f;  // (a sequence without keys: zeros)
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<uint2 *>(rows + l32 * ROWB + (((db * 4 + g) ^ (l32 % CH)) * 16) + lhi * 8) =
-            uint2{pack_bf16(acc_o[db][4 * g] * inv, acc_o[db][4 * g + 1] * inv), pack_bf16(acc_o[db][4 * g + 2] * inv, acc_o[db][4 * g + 3] * inv)};
-    asm volatile("" : : : "memory");  // the reads below are of another type (LDS accesses of a wave keep their order)
-    const uint32_t place = (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq;
-    const int cc = lane % CH;
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2 *>(rows + l32 * ROWB + (((db * 4 + g) ^ (l32 % CH)) * 16) + lhi * 8) =
+          uint2{pack_bf16(acc_o[db][4 * g] * inv, acc_o[db][4 * g + 1] * inv), pack_bf16(acc_o[db][4 * g + 2] * inv, acc_o[db][4 * g + 3] * inv)};
+  asm volatile("" : : : "memory");  // the reads below are of another type (LDS accesses of a wave keep their order)
+  const uint32_t place = (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq;
+  const int cc = lane % CH;
 #pragma unroll
-    for (int i = 0; i < 32 / RPI; ++i) {
-      const int r = RPI * i + lane / CH;
-      const uint4 v = *reinterpret_cast<const uint4 *>(rows + r * ROWB + ((cc ^ (r % CH)) * 16));
-      const uint32_t at = (uint32_t)__shfl((int)place, r, WAVE);
-      if (wave * 32 + r < nq) *(reinterpret_cast<uint4 *>((bf16_t *)a.out + (size_t)at * DH) + cc) = v;
-    }
-    return;
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int r = RPI * i + lane / CH;
+    const uint4 v = *reinterpret_cast<const uint4 *>(rows + r * ROWB + ((cc ^ (r % CH)) * 16));
+    const uint32_t at = (uint32_t)__shfl((int)place, r, WAVE);
+    if (wave * 32 + r < nq) *(reinterpret_cast<uint4 *>((bf16_t *)a.out + (size_t)at * DH) + cc) = v;
   }
-  if (wave * 32 + l32 < nq) store_partial<DH>(a, acc_o, split, (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq, lhi, n_tiles == 0, m_run, l_run);
 }
 
-template <int DH, int NW> void launch_tile(const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
-  const int q_tiles = max_q_tiles_grouped(a, 32 * NW), grid = attn_grid_grouped(a, q_tiles);
-  if (q.format == Q_E4M3) k_attn_quant_tile<DH, Q_E4M3, NW><<<grid, 64 * NW, 0, s>>>(a, q, q_tiles);
-  else k_attn_quant_tile<DH, Q_INT8, NW><<<grid, 64 * NW, 0, s>>>(a, q, q_tiles);
+template <int DH> void launch_tile(const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
+  using T = QTile<DH>;
+  const int q_tiles = max_q_tiles_grouped(a, T::BQ), grid = attn_grid_grouped(a, q_tiles);
+  if (q.format == Q_E4M3) k_attn_quant_tile<DH, Q_E4M3><<<grid, T::NT, 0, s>>>(a, q, q_tiles);
+  else k_attn_quant_tile<DH, Q_INT8><<<grid, T::NT, 0, s>>>(a, q, q_tiles);
 }
+
 // ---- merge of the splits: a wave to a (row, head), its lanes the splits' weights, then the columns -------------
+// Bound by the latency of its two dependent reads: 4 us for 32 (row, head) pairs of 8 splits.
 constexpr int MAX_SPLITS = 128;
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_quant_merge(AttnArgs a) {
@@ -778,7 +774,9 @@ template <typename T> void launch_merge(const AttnArgs &a, hipStream_t s) {
   else k_quant_merge<T, 128><<<grid, 256, 0, s>>>(a);
 }
 
-// fp32 queries and results: 16 rows x 16 lanes a workgroup, tiles of 32 keys; codes become fp32 values on their way into LDS.
+// ---- fp32 queries and results: 16 rows x 16 lanes a workgroup, tiles of 32 keys ---------------------------------
+// Codes become fp32 values on their way into LDS; every product is an fp32 one.  Bound by LDS reads, one for four products: 3882 rows of
+// 16 x 1024 keys, 32 heads of 128, 1.84 ms (35 TFLOP/s); one row of 2048 keys 50 us.
 template <int DH, int F>
 __global__ __launch_bounds__(256) void k_attn_quant_f32(AttnArgs a, QuantAttn qc) {
   typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
@@ -935,8 +933,8 @@ void launch_attention_quant(DType t, const AttnArgs &a, const QuantAttn &q, hipS
     if (a.dh == 64) launch_stream<64>(a, q, s);
     else launch_stream<128>(a, q, s);
   } else {
-    if (a.dh == 64) launch_tile<64, 4>(a, q, s);
-    else launch_tile<128, 8>(a, q, s);
+    if (a.dh == 64) launch_tile<64>(a, q, s);
+    else launch_tile<128>(a, q, s);
   }
   if (a.splits > 1) launch_merge<bf16_t>(a, s);
 }
