@@ -265,6 +265,7 @@ class Context:
         self.h = h
         self._dtype = torch.float32 if cfg.dtype == F32 else torch.bfloat16
         self._dq, self._dkv = cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+        self._dev = torch.cuda.current_device()  # where the scratch memory is
 
     def close(self):
         if getattr(self, "h", None):
@@ -371,6 +372,12 @@ class Context:
     # ---- normalised query and key heads; the cache in 8 bits.  Tensors are checked against the context: type, number of elements, device.
     # (A call takes the host about as long as a short kernel the GPU, so what it asks of torch is asked once.)
 
+    def _here(self) -> int:
+        dev = _device()
+        if dev != self._dev:
+            raise ValueError("the context is on device %d, the current one is %d" % (self._dev, dev))
+        return dev
+
     def _arg(self, t, numel, what, dev, dtype=None):
         dtype = dtype or self._dtype
         if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
@@ -415,7 +422,7 @@ class Context:
 
     def head_norm_rope(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: LayerCache, q_out):
         """qkv: [n, (H + 2 Hkv) dh], rows may be strided; g_q, g_k: [dh] or None; rows None: all B*L tokens."""
-        dev = _device()
+        dev = self._here()
         r, n = self._rows(rows, B, L, dev)
         p, ld = self._qkv(qkv, n, dev)
         q = self._arg(q_out, n * self._dq, "q_out", dev)
@@ -423,7 +430,7 @@ class Context:
                                                   L, C.byref(cache), q, _raw_stream(dev)))
 
     def head_norm_rope_quant(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: QuantCache, q_out):
-        dev = _device()
+        dev = self._here()
         r, n = self._rows(rows, B, L, dev)
         p, ld = self._qkv(qkv, n, dev)
         q = self._arg(q_out, n * self._dq, "q_out", dev)
@@ -431,14 +438,14 @@ class Context:
                                                         B, L, self._quant(cache, B, L, dev), q, _raw_stream(dev)))
 
     def quant_write(self, k, v, rows: Optional[IndexList], B, L, cache: QuantCache):
-        dev = _device()
+        dev = self._here()
         r, n = self._rows(rows, B, L, dev)
         n *= self._dkv
         self._check(self.lib.dyllm_quant_write(self.h, self._arg(k, n, "k", dev), self._arg(v, n, "v", dev), r, B, L,
                                                self._quant(cache, B, L, dev), _raw_stream(dev)))
 
     def quant_read(self, cache: QuantCache, rows: Optional[IndexList], B, L, k_out, v_out):
-        dev = _device()
+        dev = self._here()
         r, n = self._rows(rows, B, L, dev)
         n *= self._dkv
         self._check(self.lib.dyllm_quant_read(self.h, self._quant(cache, B, L, dev), r, B, L, self._arg(k_out, n, "k_out", dev),
@@ -446,7 +453,7 @@ class Context:
 
     def partial_attention_quant(self, q_sal, cache: QuantCache, rows: Optional[IndexList], B, L, c_sal_out, kv_len=None):
         """kv_len: int32 [B] device tensor (keys of each sequence) or None."""
-        dev = _device()
+        dev = self._here()
         r, n = self._rows(rows, B, L, dev)
         n *= self._dq
         self._check(self.lib.dyllm_partial_attention_quant(
@@ -455,7 +462,7 @@ class Context:
 
     def qkv_refresh_normed(self, w: LayerWeights, g_q, g_k, x, rows: Optional[IndexList], B, L, cache, q_sal_out):
         """cache: LayerCache (storage type) or QuantCache."""
-        dev = _device()
+        dev = self._here()
         r, n = self._rows(rows, B, L, dev)
         quant = isinstance(cache, QuantCache)
         self._check(self.lib.dyllm_qkv_refresh_normed(
@@ -467,7 +474,7 @@ class Context:
     def layer_step_quant(self, w: LayerWeights, g_q, g_k, cache: LayerCache, quant: QuantCache, x, idx_in: IndexList, B, L,
                          tau, idx_out: IndexList, cos_out=None, kv_len=None):
         """Of cache only c and out are used."""
-        dev = _device()
+        dev = self._here()
         i, n = self._rows(idx_in, B, L, dev)
         o, _ = self._rows(idx_out, B, L, dev)
         self._check(self.lib.dyllm_layer_step_quant(

@@ -95,7 +95,10 @@ class Layer:
         self._install(wt, packed)
 
     def set_caches(self, caches: Dict[str, np.ndarray]):
-        for name in ("k", "v", "c", "out"):
+        if self.quant is not None:  # keys and values are quantised as they come
+            k, v = (to_device(caches[n].astype(np.float32), self.dtype) for n in ("k", "v"))
+            self.ctx.quant_write(k, v, None, self.B, self.L, self.quant)
+        for name in ("k", "v", "c", "out") if self.quant is None else ("c", "out"):
             getattr(self, name).copy_(to_device(caches[name].astype(np.float32), self.dtype))
         if "lse" in caches and self.lse is not None:
             self.lse.copy_(torch.from_numpy(np.ascontiguousarray(caches["lse"], dtype=np.float32)).cuda())
@@ -132,6 +135,8 @@ class Layer:
                          idx_out: Optional[B_.IndexList] = None, want_cos: bool = True,
                          kv_len: Optional[torch.Tensor] = None):
         """A step of a layer made with `codes`; a list of all tokens with tau > 1 makes it a dense one.  kv_len: int32 [B] or None."""
+        if self.quant is None:
+            raise ValueError("the layer was made without `codes`")
         out = self.idx_out if idx_out is None else idx_out
         self.ctx.layer_step_quant(self.w, self.g_q, self.g_k, self.cache, self.quant, x_dev, idx_in, self.B, self.L, tau, out,
                                   self.cos if want_cos else None, kv_len)

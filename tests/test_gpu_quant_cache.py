@@ -406,6 +406,34 @@ def test_attention_of_many_ragged_rows(dh, Hkv, codes):
     _check_attend(59, "bf16", 28, Hkv, dh, B, L, counts, codes, kv_len=kv_len, cap=sum(counts) + 40)
 
 
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("dh,B,rows", [(128, 64, 97), (64, 104, 97), (128, 64, 2)])
+def test_attention_with_vectors_that_hold_no_number(dh, B, rows, codes):
+    """Keys, values and queries that are no numbers make NaN of the rows that meet them and leave the others as they were, in both forms."""
+    H, Hkv, L = 32, 1, 97
+    _say("attend, inf and nan", dh, B, rows, codes)
+    g = W.philox(60, dh, rows, codes)
+    ctx = _ctx("bf16", H, Hkv, dh, B, L)
+    c = _cache(g, B, L, Hkv, dh, codes)
+    idx, off, il = _lists(60, B, L, (rows,) * B)
+    q = _dev(g.standard_normal((idx.size, H, dh)), "bf16")
+    good, out = (torch.zeros(idx.size, H * dh, dtype=TD["bf16"], device="cuda") for _ in range(2))
+    ctx.partial_attention_quant(q, c, il, B, L, good)
+    c.k_scale[3, 0, 7] = c.v_scale[5, 0, 96] = float("nan")
+    want = np.zeros((idx.size, H), bool)
+    want[off[3]:off[4]] = want[off[5]:off[6]] = True
+    for b, h, x in ((8, 0, np.inf), (9, 31, np.nan), (B - 1, 17, -np.inf)):
+        q[int(off[b + 1]) - 1, h, dh - 1] = x
+        want[off[b + 1] - 1, h] = True
+    ctx.partial_attention_quant(q, c, il, B, L, out)
+    torch.cuda.synchronize()
+    lost, o, w = torch.isnan(out.view(-1, H, dh)), out.view(-1, H, dh), torch.from_numpy(want).cuda()
+    assert torch.isfinite(good).all()
+    assert torch.equal(lost.all(-1), w) and torch.equal(lost.any(-1), w)
+    assert torch.equal(o[~w], good.view(-1, H, dh)[~w])
+    ctx.close()
+
+
 def test_attention_of_all_tokens_is_the_full_list():
     t, H, Hkv, dh, B, L = "bf16", 4, 2, 128, 2, 200
     _say("attention: rows None")
@@ -585,6 +613,35 @@ def test_layer_step_stays_near_the_layer_without_codes(t):
     ds = np.abs(k).max() * 0.5 / 127 * 40.0 / math.sqrt(dh)  # (q of 64 elements about N(0, 1): |q|_1 < 80)
     assert np.max(np.abs(a - b)) <= np.abs(v).max() * (0.5 / 127 + math.expm1(2 * ds) + 4 * U[t])
     full.close(), lay.close()
+
+
+def test_caches_of_a_layer_go_in_and_out():
+    """A layer's caches set from the host are the ones read back, keys and values as the codes hold them; steps that need the other kind of cache are refused."""
+    from paper_2603_08026_amd.layer import Layer
+    B, L, t, H, Hkv, dh = 2, 50, "bf16", 4, 2, 64
+    _say("layer caches")
+    s, w = _layer(t, H, Hkv, dh, B, L, 85, False)
+    lay, plain = Layer.from_shape(s, B, L, codes="e4m3"), Layer.from_shape(s, B, L)
+    for z in (lay, plain):
+        z.set_weights(w)
+    g = W.philox(86)
+    start = {n: g.standard_normal(tuple(getattr(plain, n).shape)) for n in ("k", "v", "c", "out")}
+    lay.set_caches(start)
+    got = lay.get_caches()
+    for n in ("c", "out"):
+        assert np.array_equal(got[n], _host(_dev(start[n], t)))
+    for n in ("k", "v"):  # half a step of a code, or of its smallest step, of the rounded element
+        x = _host(_dev(start[n], t))
+        assert np.all(np.abs(got[n] - x) <= np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * _scales(x, "e4m3")[..., None]))
+    lay.set_caches(got)
+    again = lay.get_caches()
+    assert all(np.array_equal(got[n], again[n]) for n in got)
+    x, il = _dev(g.standard_normal((B * L, s.hidden)), t), _lists(1, B, L, (L, L))[2]
+    with pytest.raises(ValueError):
+        plain.layer_step_quant(x, il, 2.0)
+    with pytest.raises(Bd.DyllmError):
+        lay.layer_step(x, il, 2.0)
+    lay.close(), plain.close()
 
 
 # ---- streams, graphs --------------------------------------------------------------------------------------

@@ -94,3 +94,12 @@ def test_arguments_that_the_library_refuses(made):
     assert lib.dyllm_layer_step_quant(ctx.h, C.byref(w), None, None, C.byref(alias), C.byref(c.c), None, C.c_void_p(x.data_ptr()), C.byref(r), B, L,
                                       0.5, C.byref(out), None, s) == -1
     assert ctx.poll_status() == 0
+
+
+def test_a_context_of_another_device(made, monkeypatch):
+    ctx, rows, c, bf = made
+    monkeypatch.setattr(ctx, "_dev", 1)
+    with pytest.raises(ValueError, match="context is on device 1"):
+        ctx.partial_attention_quant(bf(2, H, DH), c, rows, B, L, bf(2, H * DH))
+    with pytest.raises(ValueError, match="context is on device 1"):
+        ctx.quant_write(bf(2, HKV, DH), bf(2, HKV, DH), rows, B, L, c)
