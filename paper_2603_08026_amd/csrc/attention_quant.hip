@@ -1,6 +1,7 @@
 // Partial (row-sparse) attention over a key/value cache of 8-bit codes: exact attention rows of listed queries against all keys of
 // their sequence, c = sum_j softmax_j(q . k_j / sqrt(dh)) v_j with k_j, v_j = code * scale.  [Sec. 3.3 salient path; Alg. 3: C_sal]
 #include "attention_common.h"
+#include <float.h>
 #include <type_traits>
 
 namespace dy {
@@ -774,111 +775,179 @@ template <typename T> void launch_merge(const AttnArgs &a, hipStream_t s) {
   else k_quant_merge<T, 128><<<grid, 256, 0, s>>>(a);
 }
 
-// ---- fp32 queries and results: 16 rows x 16 lanes a workgroup, tiles of 32 keys ---------------------------------
-// Codes become fp32 values on their way into LDS; every product is an fp32 one.  Bound by LDS reads, one for four products: 3882 rows of
-// 16 x 1024 keys, 32 heads of 128, 1.84 ms (35 TFLOP/s); one row of 2048 keys 50 us.
-template <int DH, int F>
-__global__ __launch_bounds__(256) void k_attn_quant_f32(AttnArgs a, QuantAttn qc) {
-  typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
-  constexpr int BQ = 16, BK = 32, NT = 256, STR = DH + 4, CH = DH / 16, LD = (2 * BK * CH + NT - 1) / NT, OC = DH / 64;
-  __shared__ __align__(16) float Qs[BQ][STR];
-  __shared__ __align__(16) float Ks[BK][STR];
-  __shared__ __align__(16) float Vs[BK][DH];
-  __shared__ __align__(16) float Ps[BQ][BK + 4];
-  __shared__ int tile_info[3];
-  const int tid = threadIdx.x;
-  if (tid == 0) find_tile(a, BQ, blockIdx.x, tile_info);
-  __syncthreads();
-  const int b = tile_info[0];
+// ---- fp32 queries and results: R packed rows a workgroup ------------------------------------------------------
+// dh / 16 lanes take a key, a lane 16 of its codes, and 64 / (dh / 16) keys go through a wave at a time, each group of lanes with a running
+// maximum, sum and result of its own; four waves take such steps in turn.  A lane keeps its 16 elements of the R queries and results in
+// registers, so that the loop has no LDS and no barrier: per key and row 16 products and two or three moves between neighbouring lanes for
+// the score, 16 for the result, every one in fp32; the scales join the score and the probability.  Groups and waves are merged at the end.
+// Bound by the vector ALU (R = 2: 3882 rows of 16 x 1024 keys, 32 heads of 128, 1.63 ms, 40 TFLOP/s) or by the codes' way from memory and
+// the launches (R = 1: one row of 2048 keys, 32 heads, 10.5 us).  R = 4, whose registers leave two waves a SIMD: 1.65 ms, 15.8 us.
+template <int DH, int F, int R>
+__global__ __launch_bounds__(256, 3) void k_attn_quant_f32(AttnArgs a, QuantAttn qc, int q_tiles) {
+  constexpr int CPK = DH / 16, KS = WAVE / CPK, NW = 4, U = 2;  // lanes of a key, keys of a wave's step, waves, steps in flight
+  __shared__ float part[NW][R][DH], part_ml[NW][R][2];
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+  const int c = lane % CPK, group = lane / CPK;
+  const AttnItem item = attn_work_item_grouped(a, R, q_tiles, blockIdx.x);
+  const int b = item.seq, kvh = item.kv_head, split = item.split;
   if (b < 0) return;  // uniform: no such tile
-  const int j0 = tile_info[1], nq = tile_info[2];
-  const int h = blockIdx.y, kvh = h / (a.H / a.Hkv), split = blockIdx.z;
+  const int nq = item.n, grp = a.H / a.Hkv;
+  auto place = [&](int r) {  // row * H + head of packed row r
+    const int p = item.packed + r;
+    return (uint32_t)(item.row + p / grp) * (uint32_t)a.H + (uint32_t)(kvh * grp + p % grp);
+  };
   const int Lk = keys_of(qc, a.L, b);
   const int k_lo = min(split * a.chunk, Lk), k_hi = min(Lk, k_lo + a.chunk);
   const size_t stride = (size_t)a.Hkv * DH;
-  const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH, first_s = ((size_t)b * a.Hkv + kvh) * a.L;
-  const float by = 1.0f / sqrtf((float)DH);
-  const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-  uint4 raw[LD];
-  float scale[LD];
-  auto load = [&](int k0) {  // (keys past the end: the last one again, masked later)
+  const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH + c * 16, first_s = ((size_t)b * a.Hkv + kvh) * a.L;
+  const uint8_t *kc = qc.cache.k + first, *vc = qc.cache.v + first;
+  const float *ks = qc.cache.ks + first_s, *vs = qc.cache.vs + first_s;
+  float q[R][16], acc[R][16], m_run[R], l_run[R];
+  const float sc = LOG2E / sqrtf((float)DH);  // scores are kept in the log2 domain
 #pragma unroll
-    for (int u = 0; u < LD; ++u) {
-      const int i = min(tid + NT * u, 2 * BK * CH - 1), isv = i / (BK * CH), in = i % (BK * CH);
-      const int key = min(k0 + in / CH, k_hi - 1);
-      raw[u] = *reinterpret_cast<const uint4 *>((isv ? qc.cache.v : qc.cache.k) + first + (size_t)key * stride + (in % CH) * 16);
-      scale[u] = (isv ? qc.cache.vs : qc.cache.ks)[first_s + key];
+  for (int r = 0; r < R; ++r) {  // (rows past the end: the last one again, their results are never stored)
+    const float4 *src = reinterpret_cast<const float4 *>((const float *)a.q + (size_t)place(min(r, nq - 1)) * DH + c * 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = src[i];
+      q[r][4 * i] = x.x * sc; q[r][4 * i + 1] = x.y * sc; q[r][4 * i + 2] = x.z * sc; q[r][4 * i + 3] = x.w * sc;
     }
-  };
-  if (k_lo < k_hi) load(k_lo);
-  for (int e = tid; e < BQ * DH / 4; e += NT) {
-    const int r = e / (DH / 4), c = (e % (DH / 4)) * 4;
-    *reinterpret_cast<floatx4 *>(&Qs[r][c]) = r < nq ? *reinterpret_cast<const floatx4 *>((const float *)a.q + ((size_t)(j0 + r) * a.H + h) * DH + c) * by : zero;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[r][e] = 0.f;
+    m_run[r] = -FLT_MAX;  // (finite, so that a score of -inf has the probability 0)
+    l_run[r] = 0.f;
   }
-  const int row = tid / 16, sub = tid % 16;
-  floatx4 o[OC];
+  struct Step { uint4 k, v; float ks, vs; };
+  auto key_of = [&](int n) { return k_lo + (n * NW + wave) * KS + group; };
+  auto load = [&](int n, Step &s) {  // (keys past the end: the last one again, masked later)
+    const int key = min(key_of(n), k_hi - 1);
+    s.k = *reinterpret_cast<const uint4 *>(kc + (size_t)key * stride);
+    s.v = *reinterpret_cast<const uint4 *>(vc + (size_t)key * stride);
+    s.ks = ks[key];
+    s.vs = vs[key];
+  };
+  auto values = [](const uint4 &w, float *x) {
+    q_values<F>(w.x, 1.f, x); q_values<F>(w.y, 1.f, x + 4); q_values<F>(w.z, 1.f, x + 8); q_values<F>(w.w, 1.f, x + 12);
+  };
+  const int n_steps = (k_hi - k_lo + NW * KS - 1) / (NW * KS);
+  Step next[U];
+  if (n_steps > 0) {
 #pragma unroll
-  for (int i = 0; i < OC; ++i) o[i] = zero;
-  float m_run = -INFINITY, l_run = 0.f;
-  for (int k0 = k_lo; k0 < k_hi; k0 += BK) {
-    __syncthreads();  // previous tile fully consumed (also orders the Qs fill)
+    for (int u = 0; u < U; ++u) load(u, next[u]);
+  }
+  for (int n = 0; n < n_steps; n += U) {
+    Step now[U];
 #pragma unroll
-    for (int u = 0; u < LD; ++u) {
-      const int i = tid + NT * u;
-      if (i < 2 * BK * CH) {
-        const int isv = i / (BK * CH), in = i % (BK * CH), key = in / CH, c = (in % CH) * 16;
-        float *dst = isv ? &Vs[key][c] : &Ks[key][c];
-        q_values<F>(raw[u].x, scale[u], dst);
-        q_values<F>(raw[u].y, scale[u], dst + 4);
-        q_values<F>(raw[u].z, scale[u], dst + 8);
-        q_values<F>(raw[u].w, scale[u], dst + 12);
+    for (int u = 0; u < U; ++u) now[u] = next[u];
+    if (n + U < n_steps) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) load(n + U + u, next[u]);
+    }
+    float score[U][R];
+    bool need = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[16];
+      values(now[u].k, x);
+      const bool exists = key_of(n + u) < k_hi;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float d0 = 0.f, d1 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          d0 = fmaf(q[r][e], x[e], d0);
+          d1 = fmaf(q[r][e + 1], x[e + 1], d1);
+        }
+        score[u][r] = exists ? lanes_sum<CPK>(d0 + d1) * now[u].ks : -INFINITY;
+        need = need || score[u][r] > m_run[r] + 8.0f;
       }
     }
-    __syncthreads();
-    if (k0 + BK < k_hi) load(k0 + BK);
-    floatx4 a0 = zero, a1 = zero;
+    if (__any(need)) {  // the running reference moves where a score exceeds it by more than 2^8: rare after the first steps
 #pragma unroll
-    for (int e = 0; e < DH; e += 4) {
-      const floatx4 qv = *reinterpret_cast<const floatx4 *>(&Qs[row][e]);
-      a0 += qv * *reinterpret_cast<const floatx4 *>(&Ks[sub][e]);
-      a1 += qv * *reinterpret_cast<const floatx4 *>(&Ks[sub + 16][e]);
+      for (int r = 0; r < R; ++r) {
+        float top = m_run[r];
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, score[u][r]);
+        const float corr = __builtin_amdgcn_exp2f(m_run[r] - top);
+        m_run[r] = top;
+        l_run[r] *= corr;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[r][e] *= corr;
+      }
     }
-    float s0 = (a0[0] + a0[1]) + (a0[2] + a0[3]), s1 = (a1[0] + a1[1]) + (a1[2] + a1[3]);
-    if (k0 + sub >= k_hi) s0 = -INFINITY;
-    if (k0 + sub + 16 >= k_hi) s1 = -INFINITY;
-    float mt = fmaxf(s0, s1);
 #pragma unroll
-    for (int off = 8; off > 0; off >>= 1) mt = fmaxf(mt, __shfl_xor(mt, off, 16));
-    const float m_new = fmaxf(m_run, mt);  // finite: every tile holds at least one valid key
-    const float corr = __expf(m_run - m_new);
-    const float p0 = __expf(s0 - m_new), p1 = __expf(s1 - m_new);
-    float ps = p0 + p1;
+    for (int u = 0; u < U; ++u) {
+      float x[16];
+      values(now[u].v, x);
 #pragma unroll
-    for (int off = 8; off > 0; off >>= 1) ps += __shfl_xor(ps, off, 16);
-    l_run = l_run * corr + ps;
-    m_run = m_new;
-    Ps[row][sub] = p0;
-    Ps[row][sub + 16] = p1;
-    __syncthreads();
+      for (int r = 0; r < R; ++r) {
+        const float p = __builtin_amdgcn_exp2f(score[u][r] - m_run[r]);
+        l_run[r] += p;
+        const float pv = p * now[u].vs;
 #pragma unroll
-    for (int i = 0; i < OC; ++i) o[i] *= corr;
-#pragma unroll
-    for (int kk = 0; kk < BK; kk += 4) {
-      const floatx4 p = *reinterpret_cast<const floatx4 *>(&Ps[row][kk]);
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int i = 0; i < OC; ++i) o[i] += p[x] * *reinterpret_cast<const floatx4 *>(&Vs[kk + x][64 * i + 4 * sub]);
+        for (int e = 0; e < 16; ++e) acc[r][e] = fmaf(pv, x[e], acc[r][e]);
+      }
     }
   }
-  if (row >= nq) return;
-  const bool none = k_lo >= k_hi, whole = a.splits == 1;
-  const size_t at = (((size_t)(whole ? 0 : split) * a.rows.cap + j0 + row) * a.H + h);
-  float *out = (whole ? (float *)a.out : a.part_o) + at * DH;
-  const float inv = !whole ? 1.0f : none ? 0.f : 1.0f / l_run;
+  // merge of a wave's groups: each exchange halves the elements that a lane answers for
 #pragma unroll
-  for (int i = 0; i < OC; ++i) *reinterpret_cast<floatx4 *>(out + 64 * i + 4 * sub) = o[i] * inv;
-  if (!whole && sub == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = float2{none && split == 0 ? 0.f : m_run, none && split == 0 ? 1.f : l_run};
+  for (int r = 0; r < R; ++r) {
+    float top = m_run[r];
+#pragma unroll
+    for (int off = CPK; off < WAVE; off *= 2) top = fmaxf(top, __shfl_xor(top, off, WAVE));
+    const float by = __builtin_amdgcn_exp2f(m_run[r] - top);
+    float l = l_run[r] * by;
+#pragma unroll
+    for (int off = CPK; off < WAVE; off *= 2) l += __shfl_xor(l, off, WAVE);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[r][e] *= by;
+    int col = c * 16;
+#pragma unroll
+    for (int off = WAVE / 2, half = 8; off >= CPK; off /= 2, half /= 2) {
+      const bool up = lane & off;
+#pragma unroll
+      for (int e = 0; e < half; ++e) {
+        const float keep = up ? acc[r][e + half] : acc[r][e], send = up ? acc[r][e] : acc[r][e + half];
+        acc[r][e] = keep + __shfl_xor(send, off, WAVE);
+      }
+      col += up ? half : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 16 / KS; ++e) part[wave][r][col + e] = acc[r][e];
+    if (lane == 0) {
+      part_ml[wave][r][0] = top;
+      part_ml[wave][r][1] = l;
+    }
+  }
+  __syncthreads();
+  // merge of the waves
+  const bool none = k_lo >= k_hi, whole = a.splits == 1;
+  for (int i = tid; i < nq * DH; i += 256) {
+    const int r = i / DH, col = i % DH;
+    float top = part_ml[0][r][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, part_ml[w][r][0]);
+    float o = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float by = __builtin_amdgcn_exp2f(part_ml[w][r][0] - top);
+      o = fmaf(part[w][r][col], by, o);
+      l = fmaf(part_ml[w][r][1], by, l);
+    }
+    const size_t at = place(r) + (whole ? 0 : (size_t)split * a.rows.cap * a.H);
+    if (whole) {
+      ((float *)a.out)[at * DH + col] = none ? 0.f : o / l;
+    } else {  // (a split without keys counts for nothing; where all are without, the first makes the row zero)
+      a.part_o[at * DH + col] = o;
+      if (col == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = float2{none && split == 0 ? 0.f : none ? -INFINITY : top * LN2, none && split == 0 ? 1.f : l};
+    }
+  }
+}
+
+template <int DH, int R> void launch_f32(const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
+  const int q_tiles = max_q_tiles_grouped(a, R), grid = attn_grid_grouped(a, q_tiles);
+  if (q.format == Q_E4M3) k_attn_quant_f32<DH, Q_E4M3, R><<<grid, 256, 0, s>>>(a, q, q_tiles);
+  else k_attn_quant_f32<DH, Q_INT8, R><<<grid, 256, 0, s>>>(a, q, q_tiles);
 }
 
 }  // namespace
@@ -889,25 +958,37 @@ __global__ __launch_bounds__(256) void k_attn_quant_f32(AttnArgs a, QuantAttn qc
 // so 32 rows a workgroup are taken for few rows or few sequences.  32 / 256 rows, us: 285 rows of 16 sequences, 1280 keys at most,
 // 45.6 / 71.3; 1941 rows 105 / 81; 1554 rows of 16 x 2048 keys 125 / 112; 102 rows of one sequence of 1024 13.5 / 24.5; 28 heads over 4,
 // 1137 rows of 13 x 1277 48.3 / 50.3; heads of 64 over 2, 7764 rows of 16 x 2048 78 / 55.
-// Splits pay a second launch and the partial results' way through memory, so only the 32-row form has them, where a few workgroups
+// fp32: 1 row a workgroup 7 alone and 17 for 1000 of them (heads of 64: 3.7 and 9.2), 2 rows 11 and 26 (5.2 and 13).  1 / 2 rows: 3882 rows
+// of 16 x 1024, 32 heads of 128, 2155 / 1632; 379 of 4 x 1024 249 / 167; 1 of 2048 10.5 / 12.2; heads of 64 over 4, 7580 rows of 16 x 2000
+// 558 / 400, 45 of 16 x 1500 11.9 / 15.
+// Splits pay a second launch and the partial results' way through memory, so only fp32 and the 32-row form have them, where a few workgroups
 // would read long sequences: 1 row of 32768 keys, 4 heads, 1 / 8 / 32 / 128 splits 183 / 33.6 / 19.5 / 25.2 us; one row in each of 16
-// sequences of 2048, 1 / 4 / 16 22.7 / 18.0 / 23.5; 102 rows of 1024, 32 heads, 1 / 2 13.5 / 16.7.
+// sequences of 2048, 1 / 4 / 16 22.7 / 18.0 / 23.5; 102 rows of 1024, 32 heads, 1 / 2 13.5 / 16.7; fp32, heads of 64, 1 row of 32000,
+// 1 / 8 / 32 / 128 120 / 22.8 / 13.5 / 17.6.
 void attention_quant_plan(DType t, size_t part_elems, AttnArgs *a) {
   const long grp = a->H / a->Hkv, rows = a->offsets ? ((long)a->rows.cap + a->B - 1) / a->B : a->L, packed = rows * grp;
-  const double pairs = (double)a->B * a->Hkv, d128 = a->dh == 128;
-  auto tiles = [&](int bq) { return pairs * ((packed + bq - 1) / bq); };
-  auto price = [&](double n) { return n * (d128 ? 15.5 : 8.5) / 512 > (d128 ? 7 : 5) ? n * (d128 ? 15.5 : 8.5) / 512 : (d128 ? 7.0 : 5.0); };
-  const int tall = d128 ? 256 : 128;
-  const double resident = d128 ? 256 : 512, n_tall = tiles(tall);
-  a->bq = t == F32 ? 16 : (d128 ? 28.5 : 25.0) * (n_tall > resident ? n_tall / resident : 1) < price(tiles(32)) ? tall : 32;
+  const bool d128 = a->dh == 128;
+  auto tiles = [&](int bq) { return (double)a->B * a->Hkv * ((packed + bq - 1) / bq); };
+  struct Price { double alone, each; };  // ns a key: of one workgroup, and that each adds where there are many
+  auto price_of = [&](int bq) {
+    if (t == F32) return bq == 1 ? (d128 ? Price{7, 0.017} : Price{3.7, 0.0092}) : (d128 ? Price{11, 0.026} : Price{5.2, 0.013});
+    if (bq == 32) return d128 ? Price{7, 15.5 / 512} : Price{5, 8.5 / 512};
+    return d128 ? Price{28.5, 28.5 / 256} : Price{25, 25.0 / 512};
+  };
+  auto price = [&](int bq, double n) {
+    const Price p = price_of(bq);
+    return n * p.each > p.alone ? n * p.each : p.alone;
+  };
+  const int low = t == F32 ? 1 : 32, tall = t == F32 ? 2 : d128 ? 256 : 128;
+  a->bq = price(tall, tiles(tall)) < price(low, tiles(low)) ? tall : low;
   a->splits = 1;
-  const int BK = t == F32 ? 32 : 128;  // keys that the waves of a workgroup take at a time
+  const int BK = t == F32 ? 4096 / a->dh : 128;  // keys that the waves of a workgroup take at a time
   if (t == F32 || a->bq == 32) {
-    const double n = t == F32 ? (double)a->B * a->H * ((rows + 15) / 16) : tiles(32);
+    const double n = tiles(a->bq);
     const size_t per_split = (size_t)a->rows.cap * a->H * a->dh;
     double best = 0;
     for (int s = 1; s <= MAX_SPLITS && (long)(s - 1) * BK < a->L && (s == 1 || s * per_split <= part_elems); ++s) {
-      const double ns = a->L / (double)s * price(n * s) + (s > 1 ? 3500 + 150.0 * s + 8.0 * s * per_split / 4000 : 0);
+      const double ns = a->L / (double)s * price(a->bq, n * s) + (s > 1 ? 3500 + 150.0 * s + 8.0 * s * per_split / 4000 : 0);
       if (s == 1 || ns < best) {
         best = ns;
         a->splits = s;
@@ -921,11 +1002,10 @@ void attention_quant_plan(DType t, size_t part_elems, AttnArgs *a) {
 void launch_attention_quant(DType t, const AttnArgs &a, const QuantAttn &q, hipStream_t s) {
   if (a.rows.cap <= 0) return;
   if (t == F32) {
-    const dim3 grid(max_q_tiles(a, 16), a.H, a.splits);
-    if (a.dh == 64 && q.format == Q_E4M3) k_attn_quant_f32<64, Q_E4M3><<<grid, 256, 0, s>>>(a, q);
-    else if (a.dh == 64) k_attn_quant_f32<64, Q_INT8><<<grid, 256, 0, s>>>(a, q);
-    else if (q.format == Q_E4M3) k_attn_quant_f32<128, Q_E4M3><<<grid, 256, 0, s>>>(a, q);
-    else k_attn_quant_f32<128, Q_INT8><<<grid, 256, 0, s>>>(a, q);
+    if (a.dh == 64 && a.bq == 1) launch_f32<64, 1>(a, q, s);
+    else if (a.dh == 64) launch_f32<64, 2>(a, q, s);
+    else if (a.bq == 1) launch_f32<128, 1>(a, q, s);
+    else launch_f32<128, 2>(a, q, s);
     if (a.splits > 1) launch_merge<float>(a, s);
     return;
   }

@@ -125,6 +125,16 @@ __device__ __forceinline__ void dma16_s(const void *sbase, uint32_t voff, uint32
                : "s"(lds_base), "v"(voff), "s"(sbase)
                : "memory", "m0");
 }
+// over N = 4 or 8 neighbouring lanes, in all of them
+template <int CTRL> __device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <int N> __device__ __forceinline__ float lanes_sum(float x) {
+  x += __uint_as_float(moved<0xB1>(__float_as_uint(x)));   // lanes 1 0 3 2
+  x += __uint_as_float(moved<0x4E>(__float_as_uint(x)));   // lanes 2 3 0 1
+  if (N == 8) x += __uint_as_float(moved<0x141>(__float_as_uint(x)));  // mirrored in eight
+  return x;
+}
 // lane i moves 4 bytes: LDS[lds_base + 4*i]
 __device__ __forceinline__ void dma4(const void *g, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"

@@ -40,16 +40,7 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const float *
   }
 }
 
-// over the N = 4 or 8 lanes of a vector, in all of them
-template <int CTRL> __device__ __forceinline__ uint32_t moved(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
-}
-template <int N> __device__ __forceinline__ float lanes_sum(float x) {
-  x += __uint_as_float(moved<0xB1>(__float_as_uint(x)));   // lanes 1 0 3 2
-  x += __uint_as_float(moved<0x4E>(__float_as_uint(x)));   // lanes 2 3 0 1
-  if (N == 8) x += __uint_as_float(moved<0x141>(__float_as_uint(x)));  // mirrored in eight
-  return x;
-}
+// the largest over the N lanes of a vector, in all of them
 template <int N> __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
   x = max(x, moved<0xB1>(x));
   x = max(x, moved<0x4E>(x));
