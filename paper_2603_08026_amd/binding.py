@@ -264,7 +264,8 @@ class Context:
             raise DyllmError(rc, self.lib.dyllm_strerror(rc).decode())
         self.h = h
         self._dtype = torch.float32 if cfg.dtype == F32 else torch.bfloat16
-        self._dq, self._dkv = cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+        self._dh, self._dq, self._dkv = cfg.head_dim, cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+        self._width, self._kv_shape = self._dq + 2 * self._dkv, (cfg.n_kv_heads, cfg.head_dim)
         self._dev = torch.cuda.current_device()  # where the scratch memory is
 
     def close(self):
@@ -379,15 +380,14 @@ class Context:
         return dev
 
     def _arg(self, t, numel, what, dev, dtype=None):
-        dtype = dtype or self._dtype
-        if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
-            raise ValueError("%s: a contiguous %s tensor of at least %d elements is wanted" % (what, dtype, numel))
+        if t.dtype is not (dtype or self._dtype) or t.numel() < numel or not t.is_contiguous():
+            raise ValueError("%s: a contiguous %s tensor of at least %d elements is wanted" % (what, dtype or self._dtype, numel))
         if t.get_device() != dev:
             raise ValueError("%s: not on the current device" % what)
         return t.data_ptr()
 
     def _gain(self, g, what, dev):
-        return None if g is None else self._arg(g, self.cfg.head_dim, what, dev)
+        return None if g is None else self._arg(g, self._dh, what, dev)
 
     def _lens(self, kv_len, B, dev):
         return None if kv_len is None else self._arg(kv_len, B, "kv_len", dev, torch.int32)
@@ -396,29 +396,36 @@ class Context:
         """(the list's structure or None, rows at most)"""
         if rows is None:
             return None, B * L
-        if rows.offsets.numel() < B + 1:
+        idx, offsets = rows.idx, rows.offsets
+        if offsets.numel() < B + 1:
             raise ValueError("rows: %d offsets are wanted" % (B + 1))
-        if rows.idx.get_device() != dev or rows.offsets.get_device() != dev:
+        if idx.dtype is not torch.int32 or offsets.dtype is not torch.int32:
+            raise ValueError("rows: int32 tensors are wanted")
+        if idx.get_device() != dev or offsets.get_device() != dev:
             raise ValueError("rows: not on the current device")
-        c = rows.c()
-        return C.byref(c), c.cap
+        n = idx.numel()
+        return C.byref(IndexListC(idx.data_ptr(), offsets.data_ptr(), n)), n
 
     def _quant(self, cache: QuantCache, B, L, dev):
-        if cache.shape != (B, L, self.cfg.n_kv_heads, self.cfg.head_dim):
-            raise ValueError("the 8-bit cache is %s, the call's %s"
-                             % (cache.shape, (B, L, self.cfg.n_kv_heads, self.cfg.head_dim)))
+        if cache.shape != (B, L, *self._kv_shape):
+            raise ValueError("the 8-bit cache is %s, the call's %s" % (cache.shape, (B, L, *self._kv_shape)))
         if cache.device != dev:
             raise ValueError("the 8-bit cache is not on the current device")
         return C.byref(cache.c)
 
     def _qkv(self, qkv, n, dev):
         """(pointer, row stride) of raw projections [n, (H + 2 Hkv) dh], whose rows may lie further apart than they are long"""
-        width = (self.cfg.n_heads + 2 * self.cfg.n_kv_heads) * self.cfg.head_dim
-        if qkv.dim() != 2 or qkv.shape[1] != width or qkv.shape[0] < n or qkv.stride(1) != 1 or (n > 1 and qkv.stride(0) < width):
-            raise ValueError("qkv: [%d, %d] with neighbouring columns is wanted" % (n, width))
+        shape, width = qkv.shape, self._width
+        if len(shape) != 2 or shape[1] != width or shape[0] < n:
+            raise ValueError("qkv: [%d, %d] is wanted" % (n, width))
+        ld = width
+        if not qkv.is_contiguous():
+            ld = qkv.stride(0) if shape[0] > 1 else width
+            if qkv.stride(1) != 1 or (n > 1 and ld < width):
+                raise ValueError("qkv: neighbouring columns and rows that do not overlap are wanted")
         if qkv.dtype is not self._dtype or qkv.get_device() != dev:
             raise ValueError("qkv: of another type or device than the context's")
-        return qkv.data_ptr(), qkv.stride(0) if qkv.shape[0] > 1 else width
+        return qkv.data_ptr(), ld
 
     def head_norm_rope(self, qkv, g_q, g_k, rows: Optional[IndexList], B, L, cache: LayerCache, q_out):
         """qkv: [n, (H + 2 Hkv) dh], rows may be strided; g_q, g_k: [dh] or None; rows None: all B*L tokens."""
