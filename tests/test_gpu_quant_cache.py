@@ -381,6 +381,13 @@ def test_attention_of_many_rows(codes):
     _check_attend(55, "bf16", 4, 4, 64, 2, 700, (700, 513), codes)
 
 
+@pytest.mark.parametrize("codes", ["e4m3", "int8"])
+@pytest.mark.parametrize("H,Hkv,dh", [(2, 2, 64), (2, 2, 128), (5, 1, 64), (3, 1, 128)])
+def test_attention_of_many_rows_in_fp32(H, Hkv, dh, codes):
+    """Enough rows for the form of two rows a workgroup, odd numbers of them, padded sequences."""
+    _check_attend(61, "f32", H, Hkv, dh, 4, 301, (301, 129, 300, 251), codes, kv_len=(301, 17, 0, 64), cap=1001)
+
+
 @pytest.mark.parametrize("q_size", [0.0, 30.0])
 def test_attention_of_flat_and_of_sharp_rows(q_size):
     _check_attend(56, "bf16", 4, 4, 128, 2, 900, (20, 130), "e4m3", q_size=q_size)
