@@ -366,15 +366,15 @@ template <int DH> void launch_stream(const AttnArgs &a, const QuantAttn &q, hipS
 }
 
 // ---- 256 packed query rows a workgroup (heads of 64: 128): many rows -------------------------------------------
-// Bound by instruction issue: a 32-key tile costs a SIMD 1024 cycles of matrix instructions and takes 1900, the rest being exponentials,
-// the maximum, LDS reads and the barrier.  A code is converted to bf16 once for all rows of the workgroup: each lane copies 16 codes of a
+// Bound by the wait of two waves a SIMD for each other: a 32-key tile holds 1024 cycles of matrix instructions a SIMD and takes about 1600, and
+// no pipe is full over a launch (7766 rows of 16 x 2048 keys, 32 heads: 308 to 327 us, matrix pipes 38 % busy, vector ALU 39 %, LDS 33 %).  A code is converted to bf16 once for all rows of the workgroup: each lane copies 16 codes of a
 // tile straight into LDS, several tiles ahead, converts them two tiles ahead of their use and writes them to a ring of bf16 tiles that every
 // wave reads, V by the transposing read.  A wave waits for its own copies alone, since it converts what it has copied; one barrier a tile.
 // While the vector ALU takes the exponentials of tile t and converts tile t + 2, the matrix pipe works through P V of tile t - 1 and the
 // scores of tile t + 1.  The running reference of the softmax moves only where the maximum exceeds it by 2^8, which is rare.
 // All rings repeat after six tiles and the loop is unrolled by that, so that LDS addresses are constants: 5 % (345 -> 326 us for 7766 rows
 // of 16 x 2048 keys, 32 heads).  Other shapes tried there: 128 rows, four waves, two workgroups a CU 317 us to 312; 64 rows a wave, keys of
-// its own, 373; 64 rows a wave and shared conversion 457; a barrier every second tile 330.
+// its own, 373; 64 rows a wave and shared conversion, two waves 457, four 395; a barrier every second tile 330.
 template <int DH_> struct QTile {
   static constexpr int DH = DH_, NW = DH == 128 ? 8 : 4, NT = 64 * NW, BQ = 32 * NW, TK = 32;
   static constexpr int ROWB = DH * 2, ROWK = ROWB + 16;             // bytes of a converted row; of K with a gap, so that a lane's reads differ by constants
