@@ -367,8 +367,8 @@ template <int DH> void launch_stream(const AttnArgs &a, const QuantAttn &q, hipS
 
 // ---- 256 packed query rows a workgroup (heads of 64: 128): many rows -------------------------------------------
 // Bound by the wait of two waves a SIMD for each other: a 32-key tile holds 1024 cycles of matrix instructions a SIMD and takes about 1600, and
-// no pipe is full over a launch (7766 rows of 16 x 2048 keys, 32 heads: 308 to 327 us, matrix pipes 38 % busy, vector ALU 39 %, LDS 33 %).  A code is converted to bf16 once for all rows of the workgroup: each lane copies 16 codes of a
-// tile straight into LDS, several tiles ahead, converts them two tiles ahead of their use and writes them to a ring of bf16 tiles that every
+// no pipe is full over a launch (7766 rows of 16 x 2048 keys, 32 heads: 308 to 327 us, matrix pipes 38 % busy, vector ALU 39 %, LDS 33 %).
+// A code is converted to bf16 once for all rows of the workgroup: each lane copies 16 codes of a tile straight into LDS, several tiles ahead, converts them two tiles ahead of their use and writes them to a ring of bf16 tiles that every
 // wave reads, V by the transposing read.  A wave waits for its own copies alone, since it converts what it has copied; one barrier a tile.
 // While the vector ALU takes the exponentials of tile t and converts tile t + 2, the matrix pipe works through P V of tile t - 1 and the
 // scores of tile t + 1.  The running reference of the softmax moves only where the maximum exceeds it by 2^8, which is rare.
