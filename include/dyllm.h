@@ -386,8 +386,9 @@ int dyllm_qkv_refresh_normed(dyllm_ctx *ctx, const dyllm_layer_weights *w, const
 /* One layer of SparseStep over a cache in 8 bits.  [Alg. 3 layer body]
  * = dyllm_qkv_refresh_normed(idx_in, quant) -> dyllm_partial_attention_quant -> dyllm_saliency(commit) ->
  *   dyllm_compact -> dyllm_salient_ffn(idx_out); arguments as in dyllm_layer_step.  Of `cache` only c and out are
- * used (k, v and lse may be NULL).  g_q, g_k: NULL for layers without such norms.  A dense step is one whose list
- * holds all tokens, with tau > 1. */
+ * used (k, v and lse may be NULL).  g_q, g_k: NULL for layers without such norms.  A row whose cosine is no number
+ * (its new or its cached context holds an infinity or NaN) is salient whatever tau is, unlike in dyllm_saliency: it
+ * reaches cache->out.  A dense step is one whose list holds all tokens, with tau > 1: it writes every row. */
 int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const void *g_q, const void *g_k,
                            dyllm_layer_cache *cache, dyllm_quant_cache *quant, const int32_t *kv_len, const void *x,
                            const dyllm_index_list *idx_in, int32_t B, int32_t L, float tau,

@@ -797,7 +797,7 @@ int dyllm_saliency(dyllm_ctx *ctx, const void *c_new, void *c_cache, const dyllm
     if (commit && c_new == c_cache) return fail(ctx, DYLLM_ERR_INVALID_ARG, "commit onto itself");
     r = Rows{nullptr, nullptr, B * L};
   }
-  launch_saliency(dt(ctx), c_new, c_cache, r, ctx->dq, tau, cos_out, flag_out, commit, (hipStream_t)stream);
+  launch_saliency(dt(ctx), c_new, c_cache, r, ctx->dq, tau, cos_out, flag_out, commit, 0, (hipStream_t)stream);
   return check_launch(ctx, "saliency");
 }
 
@@ -1156,7 +1156,8 @@ int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const v
   const Rows rin = rows_of(idx_in, B);
   if ((rc = enqueue_qkv_normed(ctx, w, g_q, g_k, x, rin, B, L, nullptr, quant, ctx->qs, s))) return rc;
   if ((rc = enqueue_attention_quant(ctx, ctx->qs, quant, kv_len, rin, idx_in->offsets, B, L, ctx->csal, s))) return rc;
-  launch_saliency(dt(ctx), ctx->csal, cache->c, rin, ctx->dq, tau, cos_out ? cos_out : ctx->cosb, ctx->flag, 1, s);
+  // a context that is no number is like no other: it goes on to the output, and the row leaves it again as soon as it is finite
+  launch_saliency(dt(ctx), ctx->csal, cache->c, rin, ctx->dq, tau, cos_out ? cos_out : ctx->cosb, ctx->flag, 1, 1, s);
   launch_compact(ctx->flag, rin, B, L, idx_out->idx, idx_out->offsets, idx_out->cap, ctx->status, ctx->scan, s);
   if ((rc = check_launch(ctx, "saliency / compact"))) return rc;
   Rows rout = rows_of(idx_out, B);  // (a subset of idx_in, whose capacity sizes the grids)

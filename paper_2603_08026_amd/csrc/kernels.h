@@ -105,9 +105,9 @@ void launch_oproj_finalize(const float *part, Splits splits, const void *x,
 // splits.done_to on (the rows below it were written by the GEMM's own epilogue)
 void launch_down_finalize(const float *part, Splits splits, const float *h,
                           Rows rows, int d, void *out_cache, hipStream_t s);
-// cosine of c_new[j] vs c_cache[row_j], flag = cos < tau, optional commit of the new row.
+// cosine of c_new[j] vs c_cache[row_j], flag = cos < tau (nan_flag where the cosine is no number), optional commit of the new row.
 void launch_saliency(DType t, const void *c_new, void *c_cache, Rows rows, int D, float tau,
-                     float *cos_out, uint8_t *flag_out, int commit, hipStream_t s);
+                     float *cos_out, uint8_t *flag_out, int commit, int nan_flag, hipStream_t s);
 // stable compaction over up to 1024 chained workgroups; out_offsets[b] = #selected tokens with id < b*L.
 // scan: compact_scan_words() device ints, all zero before the launch; the kernel leaves them zero.
 // Launches that share `scan` must not overlap.

@@ -333,7 +333,7 @@ __global__ __launch_bounds__(RB) void k_qkv_finalize(const float *__restrict__ p
 
 // ---- temporal cosine similarity + salient test (+ commit)  [Sec. 3.1, Sec. 3.2] ----------------
 // s = <a,b> / (max(|a|,1e-8) max(|b|,1e-8)), flag = s < tau.  The old cache row b is read before
-// the same thread overwrites the same elements with a.
+// the same thread overwrites the same elements with a.  A cosine that is no number has the flag nan_flag.
 // A row per workgroup: many small workgroups keep the loads of a CU in flight, a thread's four at a time (all of them up to 4096 bf16 or
 // 2048 fp32 columns).  HBM-bound where the rows are many: 32768 rows of 4096 bf16 columns (537 MB), compaction included, 96.5 -> 84.7
 // us, most of it by loads that leave the L2 alone; 7500 rows of 3584 24.3 -> 22.5; up to 30 MB equal.
@@ -342,7 +342,7 @@ constexpr int SAL_NT = 256;
 template <typename T>
 __global__ __launch_bounds__(SAL_NT) void k_saliency(const T *__restrict__ c_new, T *c_cache, Rows rows,
                                                       int D, float tau, float *__restrict__ cos_out,
-                                                      uint8_t *__restrict__ flag_out, int commit) {
+                                                      uint8_t *__restrict__ flag_out, int commit, int nan_flag) {
   __shared__ float red[3 * SAL_NT / WAVE];
   constexpr int N = Vec16<T>::N, AHEAD = 2;
   const int n = row_count(rows), nv = D / N;
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(SAL_NT) void k_saliency(const T *__restrict__ c_new
     if (threadIdx.x == 0) {
       const float s = dot / (fmaxf(sqrtf(na), 1e-8f) * fmaxf(sqrtf(nb), 1e-8f));
       if (cos_out) cos_out[j] = s;
-      flag_out[j] = (s < tau) ? 1 : 0;
+      flag_out[j] = (s < tau) ? 1 : s != s ? nan_flag : 0;
     }
   }
 }
@@ -629,14 +629,14 @@ void launch_qkv_finalize(DType t, const float *part, Splits splits, Rows rows, c
 inline int sal_grid(int cap) { return cap < 1 ? 1 : (cap > 65536 ? 65536 : cap); }
 
 void launch_saliency(DType t, const void *c_new, void *c_cache, Rows rows, int D, float tau,
-                     float *cos_out, uint8_t *flag_out, int commit, hipStream_t s) {
+                     float *cos_out, uint8_t *flag_out, int commit, int nan_flag, hipStream_t s) {
   if (rows.cap <= 0) return;
   if (t == F32)
     k_saliency<float><<<sal_grid(rows.cap), SAL_NT, 0, s>>>((const float *)c_new, (float *)c_cache, rows,
-                                                        D, tau, cos_out, flag_out, commit);
+                                                        D, tau, cos_out, flag_out, commit, nan_flag);
   else
     k_saliency<bf16_t><<<sal_grid(rows.cap), SAL_NT, 0, s>>>((const bf16_t *)c_new, (bf16_t *)c_cache,
-                                                         rows, D, tau, cos_out, flag_out, commit);
+                                                         rows, D, tau, cos_out, flag_out, commit, nan_flag);
 }
 
 void launch_compact(const uint8_t *flag, Rows rows, int B, int L, int32_t *out_idx,
