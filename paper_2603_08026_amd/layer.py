@@ -65,7 +65,8 @@ class Layer:
         self.cos = torch.zeros(self.rows_cap, dtype=torch.float32, device="cuda")
         self.wt: Dict[str, torch.Tensor] = {}
         self.w = None
-        self.g_q = self.g_k = None  # gains of the query and key heads' norms (weights "g_q", "g_k"), layer_step_quant
+        # gains of the query and key heads' norms (weights "g_q", "g_k"): layer_step_quant and dyllm_qkv_refresh_normed; other steps refuse them
+        self.g_q = self.g_k = None
 
     @classmethod
     def from_shape(cls, shape, batch, seq, max_rows=0, ctx=None, keep_lse=False, codes=None):
@@ -121,11 +122,18 @@ class Layer:
     def upload(self, x: np.ndarray) -> torch.Tensor:
         return to_device(x, self.dtype)
 
+    def _refuse_gains(self):
+        """For steps that know no norms of heads: they would leave them out without a word."""
+        if self.quant is None and not (self.g_q is None and self.g_k is None):
+            raise ValueError("the layer normalises its query and key heads (g_q, g_k); of the layer steps only layer_step_quant does that")
+
     def full_step(self, x_dev: torch.Tensor):
+        self._refuse_gains()
         self.ctx.full_step(self.w, self.cache, x_dev, self.B, self.L)
 
     def layer_step(self, x_dev: torch.Tensor, idx_in: B_.IndexList, tau: float,
                    idx_out: Optional[B_.IndexList] = None, want_cos: bool = True):
+        self._refuse_gains()
         out = self.idx_out if idx_out is None else idx_out
         self.ctx.layer_step(self.w, self.cache, x_dev, idx_in, self.B, self.L, tau, out,
                             self.cos if want_cos else None)
@@ -148,6 +156,7 @@ class Layer:
         """Sparse step with the approximate update of the other tokens; the context must cover B*L rows.
         cos_out: [B*L] fp32 (by token) or None; row_lo > 0: response-only step; cached_norm: reuse the
         cached softmax normalisers instead of Alg. 4's sum over all keys."""
+        self._refuse_gains()
         out = self.idx_out if idx_out is None else idx_out
         self.ctx.layer_step_approx(self.w, self.cache, x_dev, idx_in, self.B, self.L, tau, out, cos_out, row_lo,
                                    cached_norm)
@@ -180,12 +189,18 @@ class Stack:
     def make_list(self, idx, offsets, cap=None):
         return self.layers[0].make_list(idx, offsets, cap)
 
+    def _refuse_gains(self):
+        for layer in self.layers:
+            layer._refuse_gains()
+
     def full_step(self, x_dev: torch.Tensor):
+        self._refuse_gains()
         self.ctx.stack_full_step([l.w for l in self.layers], [l.cache for l in self.layers], x_dev,
                                  self.B, self.L)
 
     def stack_step(self, x_dev: torch.Tensor, idx_in: B_.IndexList, tau: float, want_cos: bool = True):
         """cos rows are strided by idx_in's capacity, as the library writes them."""
+        self._refuse_gains()
         cos = self.cos.view(-1)[:len(self.layers) * idx_in.cap] if want_cos else None
         self.ctx.stack_step([l.w for l in self.layers], [l.cache for l in self.layers], x_dev, idx_in,
                             self.B, self.L, tau, self.idx_outs, cos)
@@ -194,12 +209,14 @@ class Stack:
     def stack_step_approx(self, x_dev: torch.Tensor, idx_in: B_.IndexList, tau: float, row_lo: int = 0,
                           cos_out: Optional[torch.Tensor] = None, cached_norm: bool = False):
         """cos_out: [n_layers, B*L] fp32 (by token) or None."""
+        self._refuse_gains()
         self.ctx.stack_step_approx([l.w for l in self.layers], [l.cache for l in self.layers], x_dev, idx_in,
                                    self.B, self.L, tau, self.idx_outs, cos_out, row_lo, cached_norm)
         return self.idx_outs
 
     def denoise_step(self, sched: B_.Schedule, t: int, x_dev: torch.Tensor, decoded, carry, cand: B_.IndexList):
         """One iteration of the generation loop; returns (step kind, the list to carry or None)."""
+        self._refuse_gains()
         kind = self.ctx.denoise_step(sched, t, [l.w for l in self.layers], [l.cache for l in self.layers],
                                      x_dev, decoded, carry, self.B, self.L, cand, self.idx_outs)
         return kind, (None if kind == B_.STEP_DENSE else self.idx_outs[-1])
