@@ -105,8 +105,8 @@ typedef struct {
 /* The key/value cache in 8 bits: for every (token, key-value head) a vector of head_dim codes and one fp32
  * scale, value = code * scale.  [Sec. 5: the caches are the method's memory cost]
  *   DYLLM_E4M3  codes are OCP e4m3; the scale is 2^max(e, -100) with the smallest e for which the largest
- *               magnitude of the vector is at most 448 * 2^e.  Kernels read the exponent of such a scale
- *               alone: it has to be a power of two (or NaN).
+ *               magnitude of the vector is at most 448 * 2^e.  It has to be a power of two (or 0, or NaN;
+ *               not looked at): attention reads the exponent alone of some scales and the value of others.
  *   DYLLM_INT8  with m = max(largest magnitude, 2^-100): scale = m / 127, code = rint(x * (127 / m)).
  * A vector that holds an infinity or NaN is stored with a NaN for its scale and reads back as NaN. */
 #define DYLLM_E4M3 0

@@ -182,8 +182,17 @@ E4M3, INT8 = 0, 1
 CODES = {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
 
 
+def _powers_of_two(s: torch.Tensor) -> bool:
+    """Whether an fp32 tensor holds normal powers of two, +0 and NaN alone."""
+    bits = s.view(torch.int32)
+    whole = ((bits & ~0x7f800000) == 0) & (bits != 0x7f800000)  # neither sign nor fraction, no infinity
+    return bool((whole | torch.isnan(s)).all())
+
+
 class QuantCache:
-    """Key/value cache in 8 bits: codes k, v [B, L, Hkv, dh] (torch.float8_e4m3fn or torch.int8), scales [B, Hkv, L] fp32."""
+    """Key/value cache in 8 bits: codes k, v [B, L, Hkv, dh] (torch.float8_e4m3fn or torch.int8), scales [B, Hkv, L] fp32.
+    The scales of e4m3 codes have to be powers of two (or 0, or NaN for vectors that hold no number): attention reads the exponent alone of some.
+    Those of another kind are refused here, which waits for the GPU; not under stream capture, and not what is written into them later."""
 
     def __init__(self, k, v, k_scale, v_scale):
         if k.dtype not in CODES or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
@@ -195,6 +204,9 @@ class QuantCache:
         for t in (v, k_scale, v_scale):
             if t.device != k.device:
                 raise ValueError("the cache's tensors are on different devices")
+        if CODES[k.dtype] == E4M3 and not (k.is_cuda and torch.cuda.is_current_stream_capturing()):
+            if not (_powers_of_two(k_scale) and _powers_of_two(v_scale)):
+                raise ValueError("the scales of e4m3 codes have to be powers of two")
         self.k, self.v, self.k_scale, self.v_scale, self.format = k, v, k_scale, v_scale, CODES[k.dtype]
         self.shape, self.device = tuple(k.shape), k.get_device()
         self.c = QuantCacheC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.format)
