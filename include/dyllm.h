@@ -335,8 +335,8 @@ int dyllm_stack_full_step(dyllm_ctx *ctx, int32_t n_layers, const dyllm_layer_we
 
 /* ---- layers with normalised query and key heads; a key/value cache in 8 bits ------------------------
  * For the entry points of this section, besides the conventions above: rows == NULL means all B*L
- * tokens (row j = token j); tensors that start at no multiple of 16 bytes are refused (INVALID_ARG), scales
- * and lengths need their element's alignment only; outputs must not overlap inputs; list entries must be
+ * tokens (row j = token j); tensors that start at no multiple of 16 bytes, weights among them, are refused
+ * (INVALID_ARG), scales, lengths and cosines need their element's alignment only; outputs must not overlap inputs; list entries must be
  * token ids in [0, B*L), each of them once (not looked at). */
 
 /* RMSNorm of every query and key head, rotary embedding, and the merge of keys and values, in one pass over

@@ -556,6 +556,14 @@ int check_rows(dyllm_ctx *ctx, const dyllm_index_list *rows, int B, int L, bool 
   return DYLLM_OK;
 }
 
+// (unlike the row kernels of the other steps, k_heads reads 16 bytes of a bias at a time)
+int check_aligned(dyllm_ctx *ctx, const dyllm_layer_weights *w, bool ffn) {
+  bool bad = misaligned(w->wq) || misaligned(w->wk) || misaligned(w->wv) || misaligned(w->bq) || misaligned(w->bk) || misaligned(w->bv) ||
+             misaligned(w->g_attn);
+  if (ffn) bad = bad || misaligned(w->wo) || misaligned(w->w_gate) || misaligned(w->w_up) || misaligned(w->w_down) || misaligned(w->g_ffn);
+  return bad ? fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned weights") : DYLLM_OK;
+}
+
 int check_gains(dyllm_ctx *ctx, const void *g_q, const void *g_k) {
   if (misaligned(g_q) || misaligned(g_k)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "g_q / g_k is misaligned");
   return DYLLM_OK;
@@ -1123,6 +1131,7 @@ int dyllm_qkv_refresh_normed(dyllm_ctx *ctx, const dyllm_layer_weights *w, const
   int rc;
   Rows r;
   if ((rc = check_weights(ctx, w, true, false))) return rc;
+  if ((rc = check_aligned(ctx, w, false))) return rc;
   if (!x || !q_sal_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
   if (!cache == !quant) return fail(ctx, DYLLM_ERR_INVALID_ARG, "exactly one of cache and quant is given");
   if (quant && (rc = check_quant(ctx, quant))) return rc;
@@ -1143,6 +1152,7 @@ int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const v
   hipStream_t s = (hipStream_t)stream;
   if ((rc = check_bl(ctx, B, L))) return rc;
   if ((rc = check_weights(ctx, w, true, true))) return rc;
+  if ((rc = check_aligned(ctx, w, true))) return rc;
   if ((rc = check_quant(ctx, quant))) return rc;
   if (!cache || !cache->c || !cache->out || !x) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
   if (x == cache->out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "x aliases cache->out");
