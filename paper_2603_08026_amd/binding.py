@@ -382,7 +382,8 @@ class Context:
                                                 _stream()))
         return int(self.lib.dyllm_step_kind(C.byref(sched), t))
 
-    # ---- normalised query and key heads; the cache in 8 bits.  Tensors are checked against the context: type, number of elements, device.
+    # ---- normalised query and key heads; the cache in 8 bits.  Tensors are checked against the context: type, number of elements, device, no
+    # strides (rows of qkv excepted).  LayerWeights and LayerCache are addresses, which the caller answers for.
     # (A call takes the host about as long as a short kernel the GPU, so what it asks of torch is asked once.)
 
     def _here(self) -> int:
@@ -413,6 +414,8 @@ class Context:
             raise ValueError("rows: %d offsets are wanted" % (B + 1))
         if idx.dtype is not torch.int32 or offsets.dtype is not torch.int32:
             raise ValueError("rows: int32 tensors are wanted")
+        if not (idx.is_contiguous() and offsets.is_contiguous()):
+            raise ValueError("rows: contiguous tensors are wanted")
         if idx.get_device() != dev or offsets.get_device() != dev:
             raise ValueError("rows: not on the current device")
         n = idx.numel()
