@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -79,8 +80,9 @@ Layout make_layout(const dyllm_layer_cfg &c) {
   const size_t prow = R < 2048 ? R : 2048;
   const size_t widest = dq + 2 * dkv > d ? dq + 2 * dkv : d;
   l.part_elems = 16 * prow * dq > R * widest ? 16 * prow * dq : R * widest;
-  // (attention over the 8-bit cache: up to 128 splits of 32 rows)
-  const size_t few = 128 * (R < 32 ? R : 32) * dq;
+  // Attention over the 8-bit cache: up to 128 splits of a few rows, but no more of them than 512 workgroups of 32 rows leave.  Beyond the
+  // 231 (fp32: 412 of one row) that attention_quant_plan's prices fill the chip with, splits only add to the merge.
+  const size_t few = std::min((size_t)128 * (R < 32 ? R : 32) * dq, (size_t)512 * 32 * c.head_dim);
   l.quant_part_elems = l.part_elems > few ? l.part_elems : few;
   l.part_o = take(l.quant_part_elems * 4);
   l.part_ml = take(l.quant_part_elems / c.head_dim * 2 * 4);
