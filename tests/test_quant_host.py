@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from paper_2603_08026_amd import binding, build
+from tests.test_gpu_quant_splits import SPLIT
 
 
 @pytest.fixture(scope="module")
@@ -65,3 +66,11 @@ def test_scratch_of_a_context(probe, t, hidden, H, Hkv, dh, max_rows):
     ("f32", 4, 4, 64, 1, 32768, 1, 1, 27, 1216), ("f32", 32, 32, 128, 1, 32768, 3, 1, 5, 6560)])
 def test_plans_of_few_rows(probe, t, H, Hkv, dh, B, L, rows, bq, splits, chunk):
     assert probe("plan", t, 256, H, Hkv, dh, B, L, rows, rows) == ["%d %d %d" % (bq, splits, chunk)]
+
+
+# what the GPU tests of merged splits say that their cases run
+@pytest.mark.parametrize("t,H,Hkv,dh,B,L,rows,splits,chunk", SPLIT)
+def test_splits_of_the_merged_cases(probe, t, H, Hkv, dh, B, L, rows, splits, chunk):
+    bq, *got = probe("plan", t, 256, H, Hkv, dh, B, L, rows * B, rows * B)[0].split(" ")
+    assert [int(n) for n in got] == [splits, chunk] and int(bq) == (32 if t == "bf16" else 1)
+    assert splits > 8  # (the merge reads eight at a time)
