@@ -6,6 +6,7 @@
 
 // quant_probe CASE bf16 hidden heads kv_heads head_dim B L max_rows cap
 //   plan      rows in a tile, key splits, keys of a split of a list of `cap` entries
+//   q|k|v     K splits, rows in row tiles and splits of the rows behind them of the projections of `cap` rows
 //   scratch   floats of scratch that the GEMMs ask for, and of what attention over codes may use
 //   all rows  attention, write and read of all tokens (no list)
 //   refresh   dyllm_qkv_refresh_normed with one of its weights at an address that is no multiple of 16 bytes, weight by weight
@@ -36,6 +37,11 @@ int main(int argc, char **argv) {
     a.rows = rows_of(&in, B); a.offsets = in.offsets; a.B = B; a.L = L; a.H = H; a.Hkv = Hkv; a.dh = dh;
     attention_quant_plan(dt(ctx), ctx->quant_part_elems, &a);
     printf("%d %d %d\n", a.bq, a.splits, a.chunk);
+    return 0;
+  }
+  if (what == "q|k|v") {
+    const mm::GemmPlan p = mm::plan_on_host(mm::raw_plan_args(ctx->dq + 2 * ctx->dkv, cfg.hidden, ctx->part_elems, true, 32), cap);
+    printf("%d %d %d\n", p.sk, p.row_hi, p.sk_tail);
     return 0;
   }
   if (what == "scratch") {

@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from paper_2603_08026_amd import binding, build
+from tests.test_gpu_quant_refresh import B as BATCH, L as LENGTH, PLANS
 from tests.test_gpu_quant_splits import SPLIT
 
 
@@ -74,3 +75,9 @@ def test_splits_of_the_merged_cases(probe, t, H, Hkv, dh, B, L, rows, splits, ch
     bq, *got = probe("plan", t, 256, H, Hkv, dh, B, L, rows * B, rows * B)[0].split(" ")
     assert [int(n) for n in got] == [splits, chunk] and int(bq) == (32 if t == "bf16" else 1)
     assert splits > 8  # (the merge reads eight at a time)
+
+
+# ... and those of projections that the device plans
+@pytest.mark.parametrize("hidden,H,Hkv,dh,count,splits,tiled,tail", PLANS)
+def test_plans_of_the_refreshed_rows(probe, hidden, H, Hkv, dh, count, splits, tiled, tail):
+    assert probe("q|k|v", "bf16", hidden, H, Hkv, dh, BATCH, LENGTH, 0, count) == ["%d %d %d" % (splits, tiled, tail)]
