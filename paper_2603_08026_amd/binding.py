@@ -146,12 +146,15 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _device() -> int:
-    return torch._C._cuda_getDevice()
+    return torch.cuda.current_device()
 
 
-def _raw_stream(device: int) -> int:
-    """The current stream of a device."""
-    return torch._C._cuda_getCurrentRawStream(device)
+try:  # the handle without a Stream object around it: 0.1 us of a call's 7, the public way 1.1
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream
+except ImportError:
+    def _raw_stream(device: int) -> int:
+        """The current stream of a device."""
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def _stream() -> C.c_void_p:
