@@ -371,7 +371,10 @@ int dyllm_quant_read(dyllm_ctx *ctx, const dyllm_quant_cache *cache, const dyllm
 /* dyllm_partial_attention over the cache in 8 bits.  [Sec. 3.3 salient path; Alg. 3: C_sal]
  * kv_len: NULL, or [B] device int32: sequence b has the keys at positions [0, kv_len[b]) (clamped to [0, L]);
  * what lies behind them, padding, is never used.  The rows of a sequence without keys are zero.
- * q_sal: [count, H, dh]; c_sal_out: [count, H*dh]. */
+ * q_sal: [count, H, dh]; c_sal_out: [count, H*dh].  In bf16 contexts the probabilities (in some kernels times the value's
+ * scale) are rounded to bf16 ahead of their product with the values, as in dyllm_partial_attention; maxima and
+ * sums are held in fp32.  The kernel and its key splits are chosen by rows->cap, so lists of the same rows with another
+ * capacity may differ by these roundings, and one with far more room than rows takes longer. */
 int dyllm_partial_attention_quant(dyllm_ctx *ctx, const void *q_sal, const dyllm_quant_cache *cache,
                                   const int32_t *kv_len, const dyllm_index_list *rows, int32_t B, int32_t L,
                                   void *c_sal_out, void *stream);

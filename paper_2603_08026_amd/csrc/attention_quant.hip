@@ -243,7 +243,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_quant_stream(AttnArgs a, QuantA
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc_o[db][e] *= corr;
-        // the last tile's probabilities, whose products are still to come, belong to the old reference
+        // the last tile's probabilities, whose products are still to come, belong to the old reference.  (They are rounded to bf16 a second time;
+        // corr is below 2^-8, and with it what the rounding is worth beside the new maximum.)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const uint4 w = __builtin_bit_cast(uint4, pf[k]);
@@ -257,7 +258,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_quant_stream(AttnArgs a, QuantA
       const float neg_ref = m_run == -INFINITY ? 0.f : -m_run;
       float pe[16];
       uint32_t pw[8];
-      // the scale of the value joins the probability ahead of its one rounding; the sum is over what there was before
+      // the scale of the value joins the probability ahead of its one rounding, to the bf16 of the matrix instruction; the sum is over what there
+      // was before
       auto round_pair = [&](int i) {
         l_run += pe[2 * i] + pe[2 * i + 1];
         pw[i] = pack_bf16(pe[2 * i] * vscale[2 * i], pe[2 * i + 1] * vscale[2 * i + 1]);
@@ -384,7 +386,8 @@ template <int DH_> struct QTile {
   static constexpr int AT_K = 0, AT_V = NK * HOT_K, AT_RAW = AT_V + NV * HOT, AT_RS = AT_RAW + NR * RAW, AT_SC = AT_RS + NR * NW * 256, LDS = AT_SC + NV * 8 * TK;
   static constexpr int DB = DH / 32, KK = DH / 16, SLOTS = DB + KK;
   static_assert(NT * 16 == RAW && LDS <= (NW == 8 ? 160 : 80) * 1024 && BQ * ROWB <= LDS, "eight waves to a CU; the rows leave by way of the same memory");
-  // 32-byte pair p of value row r: the rows that a read serves at a time cover all banks once
+  // 32-byte pair p of value row r: the rows that a read serves at a time cover all banks once.  (Not so the writes of converted codes, 16 bytes a
+  // lane, 32 apart.  The counters show 0.14 to 0.18 of the active LDS cycles lost to conflicts; whose they are has not been tried.)
   __device__ static __forceinline__ int v_pair(int r, int p) { return DH == 128 ? p ^ (2 * (r & 3)) : p ^ (2 * ((r >> 1) & 1)); }
 };
 
@@ -602,7 +605,7 @@ __global__ __launch_bounds__(QTile<DH>::NT, 2) void k_attn_quant_tile(AttnArgs a
       const bool need = mx > m_run + 8.0f;
       if (__any(need)) {
         // (rare after the first tiles) the accumulator changes its reference; the half of tile t-1's probabilities whose product is still to
-        // come belongs to the old one and is scaled with it
+        // come belongs to the old one and is scaled with it (and rounded a second time, as in the kernel above)
         const float corr = need ? __builtin_amdgcn_exp2f(m_run - mx) : 1.0f;
         m_run = need ? mx : m_run;
         l_run *= corr;
@@ -625,8 +628,9 @@ __global__ __launch_bounds__(QTile<DH>::NT, 2) void k_attn_quant_tile(AttnArgs a
       floatx16 s_next;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s_next[e] = 0.f;
-      // e4m3: the row sum is taken over the rounded probabilities, the values that P V uses.  int8: the scale of the value joins the
-      // probability ahead of its one rounding, and the sum is over what there was before.
+      // Probabilities are rounded to the bf16 of the matrix instruction.  e4m3: the row sum is taken over the rounded ones, the values that
+      // P V uses, two in one instruction.  int8: the scale of the value joins the probability ahead of its one rounding, and the sum is over what
+      // there was before.
       auto round_pair = [&](int i) {
         float &ps = (i & 1) ? ps1 : ps0;
         uint32_t w;
@@ -952,7 +956,9 @@ template <int DH, int R> void launch_f32(const AttnArgs &a, const QuantAttn &q, 
 
 }  // namespace
 
-// Query tile and key splits.  The prices are fits to timed launches (heads of 128, e4m3 and int8 within 10 %), ns of a workgroup per key:
+// Query tile and key splits, of what the host knows: the list's capacity stands for its count, so a list with room for far more than it holds
+// may get the tall form and no splits: one row of 32768 keys, 32 heads, in a list of one entry 51 us, of 32768 476.
+// The prices are fits to timed launches (heads of 128, e4m3 and int8 within 10 %), ns of a workgroup per key:
 //   32 rows a workgroup   7 while each CU has one; 15.5 for the 512 that the chip holds, and so on in proportion
 //   256 rows              28.5 for the 256 that the chip holds (heads of 64: 128 rows, 25, 512 of them; the 32-row form 5 and 8.5)
 // so 32 rows a workgroup are taken for few rows or few sequences.  32 / 256 rows, us: 285 rows of 16 sequences, 1280 keys at most,
