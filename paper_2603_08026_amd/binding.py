@@ -195,7 +195,8 @@ def _powers_of_two(s: torch.Tensor) -> bool:
 class QuantCache:
     """Key/value cache in 8 bits: codes k, v [B, L, Hkv, dh] (torch.float8_e4m3fn or torch.int8), scales [B, Hkv, L] fp32.
     The scales of e4m3 codes have to be powers of two (or 0, or NaN for vectors that hold no number): attention reads the exponent alone of some.
-    Those of another kind are refused here, which waits for the GPU; not under stream capture, and not what is written into them later."""
+    Those of another kind are refused here, fresh memory that nobody has cleared among them (`empty` makes a cache of zeros).  Looking waits for the
+    GPU; it is left out under stream capture, and what is written into the scales later is not looked at."""
 
     def __init__(self, k, v, k_scale, v_scale):
         if k.dtype not in CODES or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape:
@@ -209,7 +210,7 @@ class QuantCache:
                 raise ValueError("the cache's tensors are on different devices")
         if CODES[k.dtype] == E4M3 and not (k.is_cuda and torch.cuda.is_current_stream_capturing()):
             if not (_powers_of_two(k_scale) and _powers_of_two(v_scale)):
-                raise ValueError("the scales of e4m3 codes have to be powers of two")
+                raise ValueError("the scales of e4m3 codes have to be powers of two (fresh memory: zeros)")
         self.k, self.v, self.k_scale, self.v_scale, self.format = k, v, k_scale, v_scale, CODES[k.dtype]
         self.shape, self.device = tuple(k.shape), k.get_device()
         self.c = QuantCacheC(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), self.format)

@@ -81,7 +81,7 @@ Layout make_layout(const dyllm_layer_cfg &c) {
   const size_t widest = dq + 2 * dkv > d ? dq + 2 * dkv : d;
   l.part_elems = 16 * prow * dq > R * widest ? 16 * prow * dq : R * widest;
   // Attention over the 8-bit cache: up to 128 splits of a few rows, but no more of them than 512 workgroups of 32 rows leave.  Beyond the
-  // 231 (fp32: 412 of one row) that attention_quant_plan's prices fill the chip with, splits only add to the merge.
+  // 231 to 301 (fp32: some 400 of a row or two) that attention_quant_plan's prices fill the chip with, splits only add to the merge.
   const size_t few = std::min((size_t)128 * (R < 32 ? R : 32) * dq, (size_t)512 * 32 * c.head_dim);
   l.quant_part_elems = l.part_elems > few ? l.part_elems : few;
   l.part_o = take(l.quant_part_elems * 4);
