@@ -149,7 +149,8 @@ const char *dyllm_strerror(int code);
 const char *dyllm_last_error(const dyllm_ctx *ctx);
 
 /* Copies the context's device status word (0, or DYLLM_ERR_CAPACITY if some kernel since the
- * last poll found more rows than a list's capacity and dropped the excess) to *host_status.
+ * last poll found more rows than a list's capacity and dropped the excess, or DYLLM_ERR_INVALID_ARG: see the entry
+ * points that say so) to *host_status.
  * This is the one call that synchronises `stream`. */
 int dyllm_poll_status(dyllm_ctx *ctx, int32_t *host_status, void *stream);
 
@@ -396,6 +397,91 @@ int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const v
                            dyllm_layer_cache *cache, dyllm_quant_cache *quant, const int32_t *kv_len, const void *x,
                            const dyllm_index_list *idx_in, int32_t B, int32_t L, float tau,
                            dyllm_index_list *idx_out, float *cos_out, void *stream);
+
+/* ---- requests served from pages of keys and values; attention with masked and reshaped scores ----------------------
+ * Besides the conventions at the top: tensors that start at no multiple of 16 bytes are refused (INVALID_ARG), lists, lengths,
+ * positions, slopes and documents need their element's alignment only; outputs must not overlap inputs unless said.
+ * A request (number r of R) has the tokens at positions [0, len).  The keys and values of page_size neighbouring positions lie in one
+ * page, for each key-value head one after the other; position i of request r is place i % page_size of page table[r][i / page_size],
+ * and slot = page * page_size + place names it. */
+#define DYLLM_MAX_REQUESTS 8192
+typedef struct {
+  void *k;             /* [n_pages, Hkv, page_size, dh] keys, stored AFTER the rotary embedding */
+  void *v;             /* [n_pages, Hkv, page_size, dh] */
+  int32_t *table;      /* [R, max_pages] page numbers; entries behind a request's length are not looked at */
+  int32_t n_pages;
+  int32_t page_size;   /* a power of two, 16 to 1024 */
+  int32_t max_pages;   /* entries of a table row: no request is longer than max_pages * page_size */
+} dyllm_pages;
+
+/* The rows (new tokens) of a call, grouped by request. */
+typedef struct {
+  int32_t *offsets; /* [R+1] rows offsets[r] .. offsets[r+1] are those of request r, offsets[R] = count */
+  int32_t *pos;     /* [cap] position of the row's token in its request */
+  int32_t *slot;    /* [cap] where its key and value go, or -1: nowhere */
+  int32_t cap;      /* host value; rows behind it are dropped */
+} dyllm_page_rows;
+
+/* One step of the page accounting, without a host in between: pages for what requests gain, pages back from what they lose, and the rows
+ * of the step.  Of request r: len[r] tokens before, new_len[r] after, of which the last new_rows[r] are computed in this step (a prompt's
+ * chunk, a decoded token, a block that is computed again; 0 for none).  new_len[r] < len[r] gives pages back, 0 all of them.
+ *   held = ceil(len / page_size), need = ceil(new_len / page_size).
+ *   The pool is a stack: free_list[0 .. n_free[0]), the last entry on top.  Requests in order take what they gain into table[r][held .. need): first
+ *   the pages that requests lose in this call (requests in order, a request's entries in order), then from the top of the stack.  Lost pages that
+ *   nobody takes are put onto the stack in their order.
+ *   A request that gains pages and finds too few, with all that gain and stand before it served, gets none, and neither does any behind it
+ *   that gains; the status word is then DYLLM_ERR_CAPACITY.  Its rows have the slot -1 and its length stays.  So it is with one whose new_len
+ *   exceeds max_pages * page_size.
+ * Out: rows->offsets; rows->pos, rows->slot of every row; len_out[r] = new_len[r], or len[r] where the request was not served;
+ * n_free_out[0]; the table and free_list in place.  More rows than rows->cap: the excess is dropped, offsets end at cap, and the status
+ * word is set.  Inputs stay as they are, so that a repeated call with the same inputs leaves the same; for the next step the caller takes
+ * len_out and n_free_out in their place.  Lengths are clamped to what the table can hold, rows to the new length.
+ * len, new_len, new_rows, len_out: [R].  free_list: [n_pages], each page of the pool once (not looked at).  R <= DYLLM_MAX_REQUESTS.
+ * pages->k and pages->v are not looked at; rows->cap and R may exceed the context's max_rows and max_batch. */
+int dyllm_page_plan(dyllm_ctx *ctx, const dyllm_pages *pages, int32_t R, const int32_t *len, const int32_t *new_len,
+                    const int32_t *new_rows, int32_t *free_list, const int32_t *n_free, dyllm_page_rows *rows, int32_t *len_out,
+                    int32_t *n_free_out, void *stream);
+
+/* dyllm_head_norm_rope into pages, with positions on one or several axes (time, height and width of images and video).
+ * Row j of qkv, ld, g_q, g_k and the norm: as there.  Pair p of a head's columns (p, p + dh/2) is rotated by the angle
+ *   axis_pos[axis[p]][j] * rope_theta^(-2p/dh),  axis_pos: [n_axes, rows->cap], axis: HOST array [dh/2] of values below n_axes,
+ * positions of either sign and any size.  n_axes <= 8.  axis_pos NULL: every pair takes rows->pos[j] (n_axes and axis are not looked at).
+ * q_out[j], [count, H, dh]; keys and values go to rows->slot[j].  A slot of -1 (or below) drops them; one behind the last page drops them too
+ * and sets the status word to DYLLM_ERR_INVALID_ARG.  pages->table is not looked at.  rows->cap may exceed the context's max_rows. */
+int dyllm_head_norm_rope_paged(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
+                               const dyllm_page_rows *rows, int32_t R, const int32_t *axis_pos, int32_t n_axes,
+                               const uint8_t *host_axis, const dyllm_pages *pages, void *q_out, void *stream);
+
+/* What becomes of the score x = q.k / sqrt(dh) of a query at position i and a key at position j of its sequence, in this order:
+ *   cap > 0:     x = cap * tanh(x / cap)
+ *   slopes:      x = x - slopes[h] * |i - j|                                  (h: the query head)
+ *   block > 0:   the key counts only if j / block <= i / block (1: causal order; b: tokens of a block see each other), or if
+ *                j < prefix[b] (prefixes see themselves and are seen by all)
+ *   doc:         the key counts only if doc of both tokens is the same and not negative (padding).  Any numbers in any order; where equal ones are
+ *                neighbours, keys of other documents cost no time.
+ * A row that no key counts for is zero.  Keys that do not count have no influence, infinities and NaN among them. */
+typedef struct {
+  float cap;             /* 0: none */
+  int32_t block;         /* 0: all keys count */
+  const int32_t *prefix; /* NULL or [B] (R) */
+  const float *slopes;   /* NULL or [H] */
+  const int32_t *doc;    /* NULL or [B*L]; over pages: NULL */
+} dyllm_scores;
+
+/* Attention of the rows over the keys and values of their requests' pages: row j is the query at position rows->pos[j].
+ * q: [count, H, dh]; out: [count, H*dh]; kv_len: [R] tokens of each request whose keys are in place, the new ones among them (clamped to what
+ * the table can hold).  scores: NULL for plain attention in both directions.  rows->slot is not looked at (may be NULL).  Table entries that name
+ * no page of the pool are read as its first page, and set the status word to DYLLM_ERR_INVALID_ARG.  rows->cap <= the context's max_rows;
+ * R <= DYLLM_MAX_REQUESTS.  Roundings as in dyllm_partial_attention_quant; kernel and key splits are chosen by rows->cap, R and
+ * max_pages on the host and by the lengths on the device. */
+int dyllm_paged_attention(dyllm_ctx *ctx, const void *q, const dyllm_pages *pages, const dyllm_page_rows *rows, int32_t R,
+                          const int32_t *kv_len, const dyllm_scores *scores, void *out, void *stream);
+
+/* dyllm_partial_attention with masked and reshaped scores.  kv_len: NULL, or [B] keys of each sequence (clamped to [0, L]); rows == NULL means
+ * all B*L tokens.  q_sal: [count, H, dh]; k_cache, v_cache: [B, L, Hkv, dh]; c_sal_out: [count, H*dh]. */
+int dyllm_partial_attention_masked(dyllm_ctx *ctx, const void *q_sal, const void *k_cache, const void *v_cache,
+                                   const int32_t *kv_len, const dyllm_index_list *rows, int32_t B, int32_t L,
+                                   const dyllm_scores *scores, void *c_sal_out, void *stream);
 
 /* Per-stage timing of dyllm_layer_step / dyllm_full_step for measurement.  After
  * dyllm_profile_begin the next max_calls (<= 4096) step calls on this context record a HIP event on

@@ -28,6 +28,7 @@ SYMBOLS = [
     "dyllm_stack_step", "dyllm_stack_full_step", "dyllm_pack_weight",
     "dyllm_head_norm_rope", "dyllm_head_norm_rope_quant", "dyllm_quant_write", "dyllm_quant_read",
     "dyllm_partial_attention_quant", "dyllm_qkv_refresh_normed", "dyllm_layer_step_quant",
+    "dyllm_page_plan", "dyllm_head_norm_rope_paged", "dyllm_paged_attention", "dyllm_partial_attention_masked",
     "dyllm_profile_begin", "dyllm_profile_end", "dyllm_stage_count", "dyllm_stage_name",
 ]
 
@@ -63,6 +64,19 @@ class IndexListC(C.Structure):
 class QuantCacheC(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("format", C.c_int32)]
+
+
+class PagesC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("max_pages", C.c_int32)]
+
+
+class PageRowsC(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("pos", C.c_void_p), ("slot", C.c_void_p), ("cap", C.c_int32)]
+
+
+class ScoresC(C.Structure):
+    _fields_ = [("cap", C.c_float), ("block", C.c_int32), ("prefix", C.c_void_p), ("slopes", C.c_void_p), ("doc", C.c_void_p)]
 
 
 class Schedule(C.Structure):
@@ -124,6 +138,11 @@ def load_library() -> C.CDLL:
     lib.dyllm_qkv_refresh_normed.argtypes = [vp, P(LayerWeights), vp, vp, vp, P_idx, i32, i32, P(LayerCache), P_q, vp, vp]
     lib.dyllm_layer_step_quant.argtypes = [vp, P(LayerWeights), vp, vp, P(LayerCache), P_q, vp, vp, P_idx, i32, i32, f32,
                                            P_idx, vp, vp]
+    P_pages, P_rows, P_scores = P(PagesC), P(PageRowsC), P(ScoresC)
+    lib.dyllm_page_plan.argtypes = [vp, P_pages, i32, vp, vp, vp, vp, vp, P_rows, vp, vp, vp]
+    lib.dyllm_head_norm_rope_paged.argtypes = [vp, vp, i64, vp, vp, P_rows, i32, vp, i32, C.c_char_p, P_pages, vp, vp]
+    lib.dyllm_paged_attention.argtypes = [vp, vp, P_pages, P_rows, i32, vp, P_scores, vp, vp]
+    lib.dyllm_partial_attention_masked.argtypes = [vp, vp, vp, vp, vp, P_idx, i32, i32, P_scores, vp, vp]
     lib.dyllm_profile_begin.argtypes = [vp, i32]
     lib.dyllm_profile_end.argtypes = [vp, P(f32), P(i32)]
     lib.dyllm_stage_count.argtypes = []
@@ -220,6 +239,62 @@ class QuantCache:
         """A cache of zeros."""
         c = [torch.zeros(B, L, Hkv, dh, dtype=torch.int8, device=device).view(codes) for _ in range(2)]
         return QuantCache(*c, *(torch.zeros(B, Hkv, L, dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _int32s(what: str, *tensors):
+    """Checks that tensors are contiguous int32 ones on one device, and gives their addresses."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t.dtype is not torch.int32 or not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError(what + ": contiguous int32 tensors on one device are wanted")
+    return [t.data_ptr() for t in tensors]
+
+
+class Pages:
+    """Pages of keys and values: k, v [n_pages, Hkv, page_size, dh] and the page table, int32 [R, max_pages]."""
+
+    def __init__(self, k, v, table):
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or table.dim() != 2:
+            raise ValueError("pages are two [n_pages, Hkv, page_size, dh] tensors of one type and a table [R, max_pages]")
+        if v.get_device() != k.get_device() or table.get_device() != k.get_device():
+            raise ValueError("the pages' tensors are on different devices")
+        at, = _int32s("page table", table)
+        self.k, self.v, self.table = k, v, table
+        self.shape, self.dtype, self.device, self.requests = tuple(k.shape), k.dtype, k.get_device(), table.shape[0]
+        self.c = PagesC(_ptr(k), _ptr(v), at, k.shape[0], k.shape[2], table.shape[1])
+
+    @staticmethod
+    def empty(n_pages: int, Hkv: int, page_size: int, dh: int, R: int, max_pages: int, dtype=torch.bfloat16, device="cuda") -> "Pages":
+        """Pages of zeros and a table of zeros."""
+        k, v = (torch.zeros(n_pages, Hkv, page_size, dh, dtype=dtype, device=device) for _ in range(2))
+        return Pages(k, v, torch.zeros(R, max_pages, dtype=torch.int32, device=device))
+
+
+class PageRows:
+    """The rows of a call over pages: int32 offsets [R+1], pos and slot [cap]."""
+
+    def __init__(self, offsets, pos, slot):
+        if offsets.dim() != 1 or offsets.numel() < 2 or pos.dim() != 1 or slot.shape != pos.shape:
+            raise ValueError("rows are offsets [R+1], pos and slot [cap]")
+        addresses = _int32s("rows", offsets, pos, slot)
+        self.offsets, self.pos, self.slot = offsets, pos, slot
+        self.requests, self.cap, self.device = offsets.numel() - 1, pos.numel(), offsets.get_device()
+        self.c = PageRowsC(*addresses, self.cap)
+
+    @staticmethod
+    def empty(cap: int, R: int, device="cuda") -> "PageRows":
+        return PageRows(*(torch.zeros(n, dtype=torch.int32, device=device) for n in (R + 1, cap, cap)))
+
+
+class Scores:
+    """What becomes of attention scores (dyllm_scores).  prefix: int32 [B]; slopes: fp32 [H]; doc: int32 [B, L]; device tensors or None."""
+
+    def __init__(self, cap: float = 0.0, block: int = 0, prefix=None, slopes=None, doc=None):
+        self.cap, self.block, self.prefix, self.slopes, self.doc = cap, block, prefix, slopes, doc
+        for t, dtype, what in ((prefix, torch.int32, "prefix"), (slopes, torch.float32, "slopes"), (doc, torch.int32, "doc")):
+            if t is not None and (t.dtype is not dtype or not t.is_contiguous()):
+                raise ValueError("%s: a contiguous %s tensor is wanted" % (what, dtype))
+        self.c = ScoresC(cap, block, *(None if t is None else t.data_ptr() for t in (prefix, slopes, doc)))
 
 
 def make_weights(tensors: dict) -> LayerWeights:
@@ -507,6 +582,83 @@ class Context:
             self.h, C.byref(w), self._gain(g_q, "g_q", dev), self._gain(g_k, "g_k", dev), C.byref(cache),
             self._quant(quant, B, L, dev), self._lens(kv_len, B, dev), self._arg(x, B * L * self.cfg.hidden, "x", dev), i, B, L,
             tau, o, None if cos_out is None else self._arg(cos_out, n, "cos_out", dev, torch.float32), _raw_stream(dev)))
+
+    # ---- requests over pages; masked and reshaped scores
+
+    def _pages(self, pages: Pages, dev, contents=True):
+        if pages.device != dev:
+            raise ValueError("the pages are not on the current device")
+        _, hkv, _, dh = pages.shape
+        if contents and ((hkv, dh) != self._kv_shape or pages.dtype is not self._dtype):
+            raise ValueError("the pages are of %d heads of %d, %s; the context's of %d of %d, %s" % (hkv, dh, pages.dtype, *self._kv_shape, self._dtype))
+        return C.byref(pages.c)
+
+    def _page_rows(self, rows: PageRows, dev):
+        if rows.device != dev:
+            raise ValueError("rows: not on the current device")
+        return C.byref(rows.c)
+
+    def _requests(self, R, rows: PageRows, pages: Pages):
+        if rows.requests != R or pages.requests < R:
+            raise ValueError("%d requests, %d in the rows' offsets, %d in the page table" % (R, rows.requests, pages.requests))
+        return R
+
+    def _scores(self, scores: Optional[Scores], B, L, dev):
+        if scores is None:
+            return None
+        for t, n, what in ((scores.prefix, B, "prefix"), (scores.slopes, self.cfg.n_heads, "slopes"), (scores.doc, B * L, "doc")):
+            if t is not None and (t.numel() < n or t.get_device() != dev):
+                raise ValueError("%s: %d elements on the current device are wanted" % (what, n))
+        return C.byref(scores.c)
+
+    def page_plan(self, pages: Pages, length, new_length, new_rows, free_list, n_free, rows: PageRows, length_out, n_free_out):
+        """length, new_length, new_rows, length_out: int32 [R]; free_list: int32 [n_pages]; n_free, n_free_out: int32 [1]; device tensors.
+        Of pages the table and the sizes are used."""
+        dev, i32 = self._here(), torch.int32
+        R = self._requests(length.numel(), rows, pages)
+        p, r = self._pages(pages, dev, False), self._page_rows(rows, dev)
+        self._check(self.lib.dyllm_page_plan(
+            self.h, p, R, self._arg(length, R, "length", dev, i32), self._arg(new_length, R, "new_length", dev, i32),
+            self._arg(new_rows, R, "new_rows", dev, i32), self._arg(free_list, pages.shape[0], "free_list", dev, i32),
+            self._arg(n_free, 1, "n_free", dev, i32), r, self._arg(length_out, R, "length_out", dev, i32),
+            self._arg(n_free_out, 1, "n_free_out", dev, i32), _raw_stream(dev)))
+
+    def head_norm_rope_paged(self, qkv, g_q, g_k, rows: PageRows, pages: Pages, q_out, axis_pos=None, axis=None):
+        """qkv: [cap, (H + 2 Hkv) dh], rows may be strided; g_q, g_k: [dh] or None.  axis_pos: int32 [n_axes, cap] positions with axis, the axis of
+        each of the dh / 2 pairs of columns (bytes or whole numbers), or None: rows.pos for every pair."""
+        dev = self._here()
+        n, n_axes = rows.cap, 0
+        p, ld = self._qkv(qkv, n, dev)
+        q = self._arg(q_out, n * self._dq, "q_out", dev)
+        if axis_pos is not None:
+            n_axes = axis_pos.shape[0]
+            if axis_pos.dim() != 2 or axis_pos.shape[1] != n or axis is None or len(axis) != self._dh // 2:
+                raise ValueError("axis_pos: [n_axes, %d] and an axis for each of %d pairs are wanted" % (n, self._dh // 2))
+            axis_pos, axis = self._arg(axis_pos, n_axes * n, "axis_pos", dev, torch.int32), bytes(axis)
+        else:
+            axis = None
+        self._check(self.lib.dyllm_head_norm_rope_paged(
+            self.h, p, ld, self._gain(g_q, "g_q", dev), self._gain(g_k, "g_k", dev), self._page_rows(rows, dev), rows.requests, axis_pos, n_axes,
+            axis, self._pages(pages, dev), q, _raw_stream(dev)))
+
+    def paged_attention(self, q, pages: Pages, rows: PageRows, kv_len, out, scores: Optional[Scores] = None):
+        """q: [cap, H, dh]; kv_len: int32 [R]; out: [cap, H*dh]."""
+        dev = self._here()
+        R, n = self._requests(kv_len.numel(), rows, pages), rows.cap * self._dq
+        self._check(self.lib.dyllm_paged_attention(
+            self.h, self._arg(q, n, "q", dev), self._pages(pages, dev), self._page_rows(rows, dev), R, self._lens(kv_len, R, dev),
+            self._scores(scores, R, 0, dev), self._arg(out, n, "out", dev), _raw_stream(dev)))
+
+    def partial_attention_masked(self, q_sal, k_cache, v_cache, rows: Optional[IndexList], B, L, c_sal_out, scores: Optional[Scores] = None,
+                                 kv_len=None):
+        """kv_len: int32 [B] device tensor (keys of each sequence) or None."""
+        dev = self._here()
+        r, n = self._rows(rows, B, L, dev)
+        n *= self._dq
+        kv = B * L * self._dkv
+        self._check(self.lib.dyllm_partial_attention_masked(
+            self.h, self._arg(q_sal, n, "q_sal", dev), self._arg(k_cache, kv, "k_cache", dev), self._arg(v_cache, kv, "v_cache", dev),
+            self._lens(kv_len, B, dev), r, B, L, self._scores(scores, B, L, dev), self._arg(c_sal_out, n, "c_sal_out", dev), _raw_stream(dev)))
 
     def full_step(self, w: LayerWeights, cache: LayerCache, x, B, L):
         self._check(self.lib.dyllm_full_step(self.h, C.byref(w), C.byref(cache), _ptr(x), B, L, _stream()))

@@ -46,6 +46,7 @@ struct dyllm_ctx {
   int32_t *plan, *plan_up, *plan_down, *plan_kv;
   int32_t *scan;   // words of the chained compaction kernel; all zero between calls
   float *rope;     // [max_seq, dh/2, 2]
+  uint64_t turns[64];  // what a pair of columns is turned by a position, in 2^-64 turns
   // optional per-stage timing (dyllm_profile_begin / _end)
   std::vector<hipEvent_t> *prof_events;
   int prof_max_calls, prof_calls;
@@ -639,6 +640,61 @@ int enqueue_attention_quant(dyllm_ctx *ctx, const void *q, const dyllm_quant_cac
   return check_launch(ctx, "attention over the 8-bit cache");
 }
 
+// ---- requests over pages; masked and reshaped scores ------------------------------------------------
+
+static_assert(MAX_REQUESTS == DYLLM_MAX_REQUESTS, "");
+
+int check_pages(dyllm_ctx *ctx, const dyllm_pages *p, int R, bool table, bool rows) {
+  if (!p) return fail(ctx, DYLLM_ERR_INVALID_ARG, "pages is NULL");
+  if (R <= 0) return fail(ctx, DYLLM_ERR_INVALID_ARG, "R must be positive");
+  if (R > DYLLM_MAX_REQUESTS) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "more than DYLLM_MAX_REQUESTS requests");
+  if (p->n_pages <= 0 || p->page_size <= 0 || (table && p->max_pages <= 0)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "page sizes must be positive");
+  if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
+    return fail(ctx, DYLLM_ERR_UNSUPPORTED, "page_size is no power of two from 16 to 1024");
+  if ((int64_t)p->n_pages * p->page_size > 0x7fffffff) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "slots do not fit 32 bits");
+  if (table && (int64_t)p->max_pages * p->page_size > 1 << 30) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "table rows of more than 2^30 tokens");
+  if (table && (!p->table || ((uintptr_t)p->table & 3))) return fail(ctx, DYLLM_ERR_INVALID_ARG, "the page table is NULL or misaligned");
+  if (rows && (!p->k || !p->v || misaligned(p->k) || misaligned(p->v))) return fail(ctx, DYLLM_ERR_INVALID_ARG, "the pages are NULL or misaligned");
+  return DYLLM_OK;
+}
+
+Pages pages_of(const dyllm_pages *p) {
+  Pages g;
+  g.k = p->k; g.v = p->v; g.table = p->table; g.n_pages = p->n_pages; g.max_pages = p->max_pages;
+  for (g.shift = 0; 1 << g.shift < p->page_size; ++g.shift) {}
+  return g;
+}
+
+int check_page_rows(dyllm_ctx *ctx, const dyllm_page_rows *r, bool pos, bool slot) {
+  if (!r || !r->offsets) return fail(ctx, DYLLM_ERR_INVALID_ARG, "rows is NULL");
+  if (r->cap < 0) return fail(ctx, DYLLM_ERR_INVALID_ARG, "negative row capacity");
+  if (r->cap > 1 << 30) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "row capacity over 2^30");
+  if (r->cap > 0 && ((pos && !r->pos) || (slot && !r->slot))) return fail(ctx, DYLLM_ERR_INVALID_ARG, "rows: positions or slots are NULL");
+  if (((uintptr_t)r->offsets | (pos ? (uintptr_t)r->pos : 0) | (slot ? (uintptr_t)r->slot : 0)) & 3) return fail(ctx, DYLLM_ERR_INVALID_ARG, "rows: misaligned");
+  return DYLLM_OK;
+}
+
+int check_scores(dyllm_ctx *ctx, const dyllm_scores *s, bool pages) {
+  if (!s) return DYLLM_OK;
+  if (!(s->cap >= 0.f) || isinf(s->cap)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "scores: cap is negative or no finite number");
+  if (s->block < 0) return fail(ctx, DYLLM_ERR_INVALID_ARG, "scores: negative block");
+  if (pages && s->doc) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "scores: documents over pages");
+  if (((uintptr_t)s->prefix | (uintptr_t)s->slopes | (uintptr_t)s->doc) & 3) return fail(ctx, DYLLM_ERR_INVALID_ARG, "scores: misaligned");
+  return DYLLM_OK;
+}
+
+ScoredAttn scored_args(const dyllm_ctx *ctx, const void *q, const dyllm_scores *sc, void *out) {
+  const dyllm_layer_cfg &c = ctx->cfg;
+  ScoredAttn a;
+  a.q = q; a.out = out;
+  a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.dh = c.head_dim;
+  if (sc) { a.soft_cap = sc->cap; a.block = sc->block; a.prefix = sc->prefix; a.slopes = sc->slopes; a.doc = sc->doc; }
+  a.part_o = ctx->part_o; a.part_ml = ctx->part_ml; a.part_elems = ctx->quant_part_elems;
+  a.n_split = (int32_t *)ctx->cosb;
+  a.status = ctx->status; a.bad_page_code = DYLLM_ERR_INVALID_ARG;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -702,6 +758,8 @@ int dyllm_create(const dyllm_layer_cfg *cfg, dyllm_ctx **out) {
 
   // rotary table in double precision on the host, cleared status word
   const int half = cfg->head_dim / 2;
+  for (int j = 0; j < half; ++j)
+    ctx->turns[j] = (uint64_t)(fmodl(powl((long double)cfg->rope_theta, -2.0L * j / cfg->head_dim) / 6.283185307179586476925286766559L, 1.0L) * 18446744073709551616.0L);
   std::vector<float> tab((size_t)cfg->max_seq * half * 2);
   for (int p = 0; p < cfg->max_seq; ++p)
     for (int j = 0; j < half; ++j) {
@@ -1175,6 +1233,100 @@ int dyllm_layer_step_quant(dyllm_ctx *ctx, const dyllm_layer_weights *w, const v
   Rows rout = rows_of(idx_out, B);  // (a subset of idx_in, whose capacity sizes the grids)
   if (rout.cap > idx_in->cap) rout.cap = idx_in->cap;
   return enqueue_ffn(ctx, w, x, cache->c, rout, cache->out, (size_t)B * L, s);
+}
+
+int dyllm_page_plan(dyllm_ctx *ctx, const dyllm_pages *pages, int32_t R, const int32_t *len, const int32_t *new_len,
+                    const int32_t *new_rows, int32_t *free_list, const int32_t *n_free, dyllm_page_rows *rows, int32_t *len_out,
+                    int32_t *n_free_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  if ((rc = check_pages(ctx, pages, R, true, false))) return rc;
+  if ((rc = check_page_rows(ctx, rows, true, true))) return rc;
+  if (!len || !new_len || !new_rows || !free_list || !n_free || !len_out || !n_free_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL list");
+  if (((uintptr_t)len | (uintptr_t)new_len | (uintptr_t)new_rows | (uintptr_t)free_list | (uintptr_t)n_free | (uintptr_t)len_out | (uintptr_t)n_free_out) & 3)
+    return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned list");
+  const size_t words = (size_t)R * 4;
+  for (const int32_t *in : {len, new_len, new_rows})
+    if (overlap(in, words, len_out, words) || overlap(in, words, n_free_out, 4) || overlap(in, words, rows->offsets, words + 4))
+      return fail(ctx, DYLLM_ERR_INVALID_ARG, "an output overlaps an input");
+  if (n_free == n_free_out || overlap(n_free, 4, len_out, words)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "an output overlaps an input");
+  PagePlan a;
+  a.len = len; a.new_len = new_len; a.new_rows = new_rows; a.n_free = n_free; a.free_list = free_list;
+  a.offsets = rows->offsets; a.pos = rows->pos; a.slot = rows->slot; a.len_out = len_out; a.n_free_out = n_free_out; a.status = ctx->status;
+  a.R = R; a.cap = rows->cap; a.overflow_code = DYLLM_ERR_CAPACITY;
+  launch_page_plan(pages_of(pages), a, (hipStream_t)stream);
+  return check_launch(ctx, "page plan");
+}
+
+int dyllm_head_norm_rope_paged(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
+                               const dyllm_page_rows *rows, int32_t R, const int32_t *axis_pos, int32_t n_axes,
+                               const uint8_t *host_axis, const dyllm_pages *pages, void *q_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  if (!qkv || !q_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(qkv) || misaligned(q_out) || ((uintptr_t)axis_pos & 3)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_gains(ctx, g_q, g_k))) return rc;
+  if ((rc = check_pages(ctx, pages, R, false, true))) return rc;
+  if ((rc = check_page_rows(ctx, rows, !axis_pos, true))) return rc;
+  if (ld < ctx->dq + 2 * ctx->dkv || ld * (int64_t)ctx->esz % 16) return fail(ctx, DYLLM_ERR_BAD_SHAPE, "ld is too small or no multiple of 16 bytes");
+  PagedHeads a;
+  const int half = ctx->cfg.head_dim / 2;
+  memset(a.axis, 0, sizeof(a.axis));
+  if (axis_pos) {
+    if (n_axes <= 0 || n_axes > 8 || !host_axis) return fail(ctx, DYLLM_ERR_INVALID_ARG, "n_axes is not from 1 to 8, or axis is NULL");
+    for (int p = 0; p < half; ++p) {
+      if (host_axis[p] >= n_axes) return fail(ctx, DYLLM_ERR_INVALID_ARG, "axis names an axis that there is not");
+      a.axis[p] = host_axis[p];
+    }
+  }
+  memcpy(a.turns, ctx->turns, sizeof(a.turns));
+  a.qkv = qkv; a.ld = (size_t)ld; a.g_q = g_q; a.g_k = g_k; a.eps = ctx->cfg.rms_eps;
+  a.rows = Rows{nullptr, rows->offsets + R, rows->cap};
+  a.pos = axis_pos ? axis_pos : rows->pos; a.slot = rows->slot;
+  a.H = ctx->cfg.n_heads; a.Hkv = ctx->cfg.n_kv_heads;
+  a.pages = pages_of(pages); a.q_out = q_out;
+  a.status = ctx->status; a.bad_slot_code = DYLLM_ERR_INVALID_ARG;
+  launch_heads_paged(dt(ctx), a, ctx->cfg.head_dim, (hipStream_t)stream);
+  return check_launch(ctx, "head norm, pages");
+}
+
+int dyllm_paged_attention(dyllm_ctx *ctx, const void *q, const dyllm_pages *pages, const dyllm_page_rows *rows, int32_t R,
+                          const int32_t *kv_len, const dyllm_scores *scores, void *out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  if (!q || !out || !kv_len) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(q) || misaligned(out) || ((uintptr_t)kv_len & 3)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_pages(ctx, pages, R, true, true))) return rc;
+  if ((rc = check_page_rows(ctx, rows, true, false))) return rc;
+  if ((rc = check_scores(ctx, scores, true))) return rc;
+  if (rows->cap > ctx->rows_cap) return fail(ctx, DYLLM_ERR_CAPACITY, "row capacity exceeds the context's max_rows");
+  ScoredAttn a = scored_args(ctx, q, scores, out);
+  a.pages = pages_of(pages);
+  a.kv_len = kv_len; a.offsets = rows->offsets; a.at = rows->pos; a.cap = rows->cap;
+  a.B = R; a.L = pages->max_pages << a.pages.shift;
+  scored_plan(dt(ctx), &a);
+  launch_attention_scored(dt(ctx), a, (hipStream_t)stream);
+  return check_launch(ctx, "paged attention");
+}
+
+int dyllm_partial_attention_masked(dyllm_ctx *ctx, const void *q_sal, const void *k_cache, const void *v_cache,
+                                   const int32_t *kv_len, const dyllm_index_list *rows, int32_t B, int32_t L,
+                                   const dyllm_scores *scores, void *c_sal_out, void *stream) {
+  if (!ctx) return DYLLM_ERR_INVALID_ARG;
+  int rc;
+  Rows r;
+  if (!q_sal || !k_cache || !v_cache || !c_sal_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
+  if (misaligned(q_sal) || misaligned(k_cache) || misaligned(v_cache) || misaligned(c_sal_out) || ((uintptr_t)kv_len & 3))
+    return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
+  if ((rc = check_rows(ctx, rows, B, L, true, &r))) return rc;
+  if ((rc = check_scores(ctx, scores, false))) return rc;
+  ScoredAttn a = scored_args(ctx, q_sal, scores, c_sal_out);
+  a.k = k_cache; a.v = v_cache; a.kv_len = kv_len;
+  a.offsets = rows ? rows->offsets : nullptr; a.at = r.idx; a.cap = r.cap;
+  a.B = B; a.L = L;
+  scored_plan(dt(ctx), &a);
+  launch_attention_scored(dt(ctx), a, (hipStream_t)stream);
+  return check_launch(ctx, "masked attention");
 }
 
 }  // extern "C"

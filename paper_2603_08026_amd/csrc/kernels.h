@@ -155,6 +155,40 @@ void launch_heads(DType t, const HeadsArgs &a, bool sums, int dh, int to, hipStr
 // k_out[j], v_out[j] = the cached rows row_j, code * scale rounded to T
 void launch_quant_read(DType t, const QuantCache &c, int format, Rows rows, int L, int Hkv, int dh, void *k_out, void *v_out, hipStream_t s);
 
+// ---- requests over pages of keys and values (pageops.hip) -------------------------------------------
+// [n_pages, Hkv, 1 << shift, dh] keys and values, [R, max_pages] page numbers
+struct Pages {
+  void *k = nullptr, *v = nullptr;
+  int32_t *table = nullptr;
+  int n_pages = 0, shift = 0, max_pages = 0;
+};
+// the page accounting of a step (dyllm_page_plan); words of R, R, R, n_pages and 1 in, of R + 1, cap, cap, R and 1 out
+struct PagePlan {
+  const int32_t *len, *new_len, *new_rows, *n_free;
+  int32_t *free_list, *offsets, *pos, *slot, *len_out, *n_free_out, *status;
+  int R, cap;
+  int overflow_code;
+};
+constexpr int MAX_REQUESTS = 8192;  // of a plan: their sums lie in LDS
+void launch_page_plan(const Pages &pages, const PagePlan &a, hipStream_t s);
+// RMSNorm of query and key heads, rotation with positions on several axes, keys and values into the rows' slots
+struct PagedHeads {
+  const void *qkv = nullptr;  // [cap, (H + 2 Hkv) dh], rows ld elements apart
+  size_t ld = 0;
+  const void *g_q = nullptr, *g_k = nullptr;
+  float eps = 0.f;
+  Rows rows{};                // count and capacity
+  const int32_t *pos = nullptr, *slot = nullptr;  // pos: [axes, cap]
+  int H = 0, Hkv = 0;
+  Pages pages;
+  void *q_out = nullptr;
+  int32_t *status = nullptr;
+  int bad_slot_code = 0;
+  uint64_t turns[64];         // of every pair: turns a position, in 2^-64 turns (whole turns left out)
+  uint8_t axis[64];           // ... and the axis of its positions
+};
+void launch_heads_paged(DType t, const PagedHeads &a, int dh, hipStream_t s);
+
 // ---- attention ---------------------------------------------------------------------------------
 struct AttnArgs {
   const void *q;        // [cap, H, dh] T-typed; with q_by_token: [T, H, dh], row of query j = rows.idx[j]
@@ -198,6 +232,30 @@ struct QuantAttn {
 };
 void launch_attention_quant(DType t, const AttnArgs &a, const QuantAttn &q, hipStream_t s);
 void attention_quant_plan(DType t, size_t part_elems, AttnArgs *a);
+// rows over pages (pages.table) or over [B, L] caches (k, v), with masked and reshaped scores (dyllm_scores).  Into out.
+struct ScoredAttn {
+  const void *q = nullptr, *k = nullptr, *v = nullptr;
+  void *out = nullptr;
+  Pages pages;                     // table == nullptr: k, v are [B, L, Hkv, dh]
+  const int32_t *kv_len = nullptr; // [B] or nullptr: every sequence has L keys
+  const int32_t *offsets = nullptr;  // [B+1], or nullptr: every sequence has L rows, row j at position j % L
+  const int32_t *at = nullptr;     // [cap] the rows' positions (pages) or token ids b*L + i; nullptr with offsets
+  int cap = 0, B = 0, L = 0, H = 0, Hkv = 0, dh = 0;  // (pages: L = keys that a row of the table has room for)
+  float soft_cap = 0.f;
+  int block = 0;
+  const int32_t *prefix = nullptr, *doc = nullptr;
+  const float *slopes = nullptr;
+  // scratch: partial results of key splits [splits, cap, H, dh] and their (maximum, sum), splits of every row
+  float *part_o = nullptr, *part_ml = nullptr;
+  int32_t *n_split = nullptr;
+  size_t part_elems = 0;
+  int32_t *status = nullptr;
+  int bad_page_code = 0;
+  // chosen by scored_plan: rows of a tile, most splits of a sequence, workgroups to split for
+  int bq = 0, splits = 1, target = 0;
+};
+void scored_plan(DType t, ScoredAttn *a);
+void launch_attention_scored(DType t, const ScoredAttn &a, hipStream_t s);
 // exact rows (a) and the context update of Alg. 4 (b: norm_k) in one launch, where both are bf16 with head_dim 128, one key split
 // and the same query tile: returns whether they were launched
 bool launch_attention_both(const AttnArgs &a, const AttnArgs &b, hipStream_t s);

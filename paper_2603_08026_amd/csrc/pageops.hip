@@ -1,0 +1,289 @@
+// Requests over pages of keys and values: the page accounting of a step, and the pass over raw projections that writes keys and values into the
+// rows' slots.
+#include <type_traits>
+#include "attention_common.h"
+#include "common.h"
+#include "kernels.h"
+
+namespace dy {
+
+namespace {
+
+// ---- page accounting ------------------------------------------------------------------------------------
+// held = ceil(len / P), need = ceil(new_len / P); loss = held - need and gain = need - held where positive.  Three prefix sums over the
+// requests (rows, gains, losses) say everything: released page k is entry need + k - (losses before) of the request it falls into, taken
+// page k is released page k while there are any and then comes from the top of the free list, and a row's slot needs the one page its
+// position lies in.  So the sums are made once a workgroup, in LDS, and rows, taken pages and pages that go back to the list are dealt out
+// by their numbers, each finding its request by a binary search: no workgroup waits for another, long prompts are shared out, and the
+// result does not depend on the order of anything.
+// Bound by the launch and the chain load - scan - search - store.
+constexpr int PLAN_NT = 1024;
+constexpr int MANY = 1 << 30;  // sums stop here
+__device__ __forceinline__ int sat(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)MANY); }
+__device__ __forceinline__ int sat_scan(int x) {  // inclusive over a wave
+  const int lane = threadIdx.x % WAVE;
+#pragma unroll
+  for (int o = 1; o < WAVE; o *= 2) {
+    const int y = __shfl_up(x, o, WAVE);
+    if (lane >= o) x = sat(x, y);
+  }
+  return x;
+}
+// first r with v[r] > k, v ascending; n if none
+__device__ __forceinline__ int first_above(const int *v, int n, int k) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int m = (lo + hi) >> 1;
+    if (v[m] > k) hi = m; else lo = m + 1;
+  }
+  return lo;
+}
+
+template <int MOST>
+__global__ __launch_bounds__(PLAN_NT) void k_page_plan(Pages pages, PagePlan a) {
+  __shared__ int sums[3 * MOST];  // inclusive sums [R] of rows, gains, losses
+  __shared__ int wave_total[3][PLAN_NT / WAVE], taken_of[PLAN_NT / WAVE];
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, R = a.R;
+  int *rows_to = sums, *gain_to = sums + R, *loss_to = sums + 2 * R;
+  const int shift = pages.shift;
+  const long room = (long)pages.max_pages << shift;  // (below 2^31: checked on the host)
+  struct Req { int len, then, rows, held, need; bool fits; };
+  auto request = [&](int r) {
+    Req q;
+    q.len = (int)min((long)max(a.len[r], 0), room);
+    const int want = max(a.new_len[r], 0);
+    q.fits = want <= room;
+    q.then = q.fits ? want : q.len;
+    q.rows = min(max(a.new_rows[r], 0), q.then);
+    q.held = (int)(((long)q.len + (1 << shift) - 1) >> shift);
+    q.need = (int)(((long)q.then + (1 << shift) - 1) >> shift);
+    return q;
+  };
+  int carry[3] = {0, 0, 0};
+  bool unfit = false;
+  for (int r0 = 0; r0 < R; r0 += PLAN_NT) {
+    const int r = r0 + tid;
+    int x[3] = {0, 0, 0};
+    if (r < R) {
+      const Req q = request(r);
+      x[0] = min(q.rows, MANY);
+      x[1] = max(q.need - q.held, 0);
+      x[2] = max(q.held - q.need, 0);
+      unfit = unfit || !q.fits;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) x[i] = sat_scan(x[i]);
+    __syncthreads();
+    if (lane == WAVE - 1)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) wave_total[i][wave] = x[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {  // (the totals of 16 waves, summed up by every wave)
+      const int t = lane < PLAN_NT / WAVE ? wave_total[i][lane] : 0;
+      const int upto = sat_scan(t);
+      const int before = wave ? __builtin_amdgcn_readlane(upto, __builtin_amdgcn_readfirstlane(wave) - 1) : 0;
+      if (r < R) sums[i * R + r] = sat(sat(carry[i], before), x[i]);
+      carry[i] = sat(carry[i], __builtin_amdgcn_readlane(upto, PLAN_NT / WAVE - 1));
+    }
+  }
+  __syncthreads();
+  const int n_rows = carry[0], released = carry[2], n_free = min(max(a.n_free[0], 0), pages.n_pages);
+  const int have = sat(n_free, released);
+  // pages taken: the gains of the served requests, which are a prefix of those that gain
+  int taken = 0;
+  for (int r = tid; r < R; r += PLAN_NT) {
+    const int to = gain_to[r];
+    if (to <= have) taken = max(taken, to);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) taken = max(taken, __shfl_xor(taken, o, WAVE));
+  if (lane == 0) taken_of[wave] = taken;
+  __syncthreads();
+  taken = taken_of[0];
+#pragma unroll
+  for (int w = 1; w < PLAN_NT / WAVE; ++w) taken = max(taken, taken_of[w]);
+
+  const bool short_of_pages = carry[1] > have, excess = n_rows > a.cap;
+  if ((short_of_pages || excess || unfit) && (blockIdx.x == 0 || unfit)) {
+    if (lane == 0 || unfit) *a.status = a.overflow_code;
+  }
+  const int step = gridDim.x * PLAN_NT, first = blockIdx.x * PLAN_NT + tid;
+  auto released_page = [&](int k) {
+    const int r = first_above(loss_to, R, k);
+    const Req q = request(r);
+    return pages.table[(size_t)r * pages.max_pages + q.need + (k - (r ? loss_to[r - 1] : 0))];
+  };
+  auto taken_page = [&](int k) { return k < released ? released_page(k) : a.free_list[n_free - 1 - (k - released)]; };
+  auto served = [&](int r) {
+    const int before = r ? gain_to[r - 1] : 0;
+    return gain_to[r] == before || gain_to[r] <= have;
+  };
+  // rows
+  for (int j = first; j < min(n_rows, a.cap); j += step) {
+    const int r = first_above(rows_to, R, j), before = r ? rows_to[r - 1] : 0;
+    const Req q = request(r);
+    const int p = q.then - q.rows + (j - before), e = p >> shift;
+    a.pos[j] = p;
+    int slot = -1;
+    if (q.fits && served(r)) {
+      const int page = e < q.held ? pages.table[(size_t)r * pages.max_pages + e] : taken_page((r ? gain_to[r - 1] : 0) + (e - q.held));
+      slot = (int)(((uint32_t)page << shift) | (uint32_t)(p & ((1 << shift) - 1)));
+    }
+    a.slot[j] = slot;
+  }
+  // table entries gained
+  for (int k = first; k < taken; k += step) {
+    const int r = first_above(gain_to, R, k);
+    const Req q = request(r);
+    pages.table[(size_t)r * pages.max_pages + q.held + (k - (r ? gain_to[r - 1] : 0))] = taken_page(k);
+  }
+  // pages that go back
+  for (int k = taken + first; k < released; k += step) {
+    const int to = n_free + (k - taken);
+    if (to < pages.n_pages) a.free_list[to] = released_page(k);
+  }
+  for (int r = first; r < R; r += step) {
+    const Req q = request(r);
+    a.len_out[r] = q.fits && served(r) ? q.then : q.len;
+    a.offsets[r + 1] = min(rows_to[r], a.cap);
+  }
+  if (first == 0) {
+    a.offsets[0] = 0;
+    a.n_free_out[0] = min(have - taken, pages.n_pages);
+  }
+}
+
+// ---- head norms, rotation on several axes, keys and values into slots ---------------------------------------------
+// As k_heads (headops.hip) takes a head: dh / 16 lanes, 8 neighbouring columns of each half a lane.  Here a wave takes `per` groups of
+// heads of one row, and with them the row's angles once: a lane computes cosine and sine of one pair and leaves them in LDS.
+//   angle = pos * f turns, f = theta^(-2p/dh) / 2 pi, held in 2^-64 turns: the product modulo 2^64 is the angle's fraction of a turn with whole
+// turns gone, exact to 2^-33 turns at any 32-bit position.  Its nearest quarter turn leaves |x| <= pi / 4, where the series of sine and
+// cosine end with x^9 and x^10 (what is left out is below 2e-9 and 2e-10).
+__device__ __forceinline__ float2 cos_sin(uint64_t f, int pos) {
+  const uint32_t t = (uint32_t)((f * (uint64_t)(int64_t)pos) >> 32);
+  const uint32_t q = (t + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(t - (q << 30)) * 1.46291807926715968e-9f;  // 2 pi / 2^32
+  const float y = x * x;
+  const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), x);
+  const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.75573192e-7f, 2.48015873e-5f), -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.0f);
+  const float co = q & 1 ? s : c, si = q & 1 ? c : s;
+  return float2{(q + 1) & 2 ? -co : co, q & 2 ? -si : si};
+}
+
+template <typename T> __device__ __forceinline__ void load8(const T *p, float *x) {
+  constexpr int N = Vec16<T>::N;
+#pragma unroll
+  for (int i = 0; i < 8 / N; ++i) {
+    const Vec16<T> v = ld16(p + i * N);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[i * N + e] = v.get(e);
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, const float *x) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4 *>(p) = uint4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+  } else {
+    *reinterpret_cast<float4 *>(p) = float4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<float4 *>(p + 4) = float4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+constexpr int PH_NT = 256, PH_WAVES = PH_NT / WAVE;
+
+template <typename T, int DH>
+__global__ __launch_bounds__(PH_NT) void k_heads_paged(PagedHeads a, int per, int parts) {
+  constexpr int LPH = DH / 16, HPW = WAVE / LPH, HALF = DH / 2;
+  __shared__ float2 table[PH_WAVES][HALF];
+  const int n = min(*a.rows.count, a.rows.cap);
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, sub = lane % LPH;
+  const int HT = a.H + 2 * a.Hkv, P = 1 << a.pages.shift;
+  const long slots = (long)a.pages.n_pages << a.pages.shift;
+  const uint32_t items = (uint32_t)n * (uint32_t)parts;
+  for (uint32_t it = blockIdx.x * PH_WAVES + wave; it < items; it += gridDim.x * PH_WAVES) {
+    const int j = (int)(it / (uint32_t)parts), g0 = (int)(it % (uint32_t)parts) * per;
+    const int slot = a.slot[j];
+    if (lane < HALF) table[wave][lane] = cos_sin(a.turns[lane], a.pos[(size_t)a.axis[lane] * a.rows.cap + j]);
+    if (slot >= slots && lane == 0) *a.status = a.bad_slot_code;
+    const bool keep = slot >= 0 && slot < slots;
+    const size_t page = (size_t)((uint32_t)slot >> a.pages.shift), place = (uint32_t)slot & (P - 1);
+    __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses keep their order)
+    float co[8], si[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float2 cs = table[wave][8 * sub + e];
+      co[e] = cs.x; si[e] = cs.y;
+    }
+    __builtin_amdgcn_wave_barrier();
+    const T *row = (const T *)a.qkv + (size_t)j * a.ld + 8 * sub;
+    for (int g = g0; g < g0 + per; ++g) {
+      const int head = g * HPW + lane / LPH;
+      if (head >= HT) break;  // (whole groups of lanes)
+      const int kind = head < a.H ? 0 : head < a.H + a.Hkv ? 1 : 2;  // q, k, v
+      float x1[8], x2[8];
+      load8(row + (size_t)head * DH, x1);
+      load8(row + (size_t)head * DH + HALF, x2);
+      if (kind < 2) {
+        const T *gain = (const T *)(kind == 0 ? a.g_q : a.g_k);
+        if (gain) {
+          float ss = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ss = fmaf(x2[e], x2[e], fmaf(x1[e], x1[e], ss));
+          const float by = 1.0f / sqrtf(lanes_sum<LPH>(ss) * (1.0f / DH) + a.eps);
+          float g1[8], g2[8];
+          load8(gain + 8 * sub, g1);
+          load8(gain + 8 * sub + HALF, g2);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { x1[e] *= by * g1[e]; x2[e] *= by * g2[e]; }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = x1[e], q = x2[e];
+          x1[e] = rotated(p, co[e], -(q * si[e]));
+          x2[e] = rotated(q, co[e], p * si[e]);
+        }
+      }
+      T *dst;
+      if (kind == 0) {
+        dst = (T *)a.q_out + ((size_t)j * a.H + head) * DH;
+      } else {
+        if (!keep) continue;
+        const int h = head - a.H - (kind == 2 ? a.Hkv : 0);
+        dst = (T *)(kind == 1 ? a.pages.k : a.pages.v) + ((page * a.Hkv + h) * P + place) * DH;
+      }
+      store8(dst + 8 * sub, x1);
+      store8(dst + 8 * sub + HALF, x2);
+    }
+  }
+}
+
+}  // namespace
+
+void launch_page_plan(const Pages &pages, const PagePlan &a, hipStream_t s) {
+  const long work = (long)a.cap + a.R;
+  const long blocks = (work + 2 * PLAN_NT - 1) / (2 * PLAN_NT);
+  const int grid = (int)(blocks < 1 ? 1 : blocks > 256 ? 256 : blocks);
+  if (a.R <= 1024) k_page_plan<1024><<<grid, PLAN_NT, 0, s>>>(pages, a);
+  else k_page_plan<MAX_REQUESTS><<<grid, PLAN_NT, 0, s>>>(pages, a);
+}
+
+void launch_heads_paged(DType t, const PagedHeads &a, int dh, hipStream_t s) {
+  if (a.rows.cap <= 0) return;
+  const int hpw = WAVE / (dh / 16), groups = (a.H + 2 * a.Hkv + hpw - 1) / hpw;
+  // groups of a wave: as many as leave the chip its waves
+  long per = (long)a.rows.cap * groups / 8192;
+  per = per < 1 ? 1 : per > groups ? groups : per;
+  const int parts = (int)((groups + per - 1) / per);
+  per = (groups + parts - 1) / parts;
+  const uint64_t blocks = ((uint64_t)a.rows.cap * parts + PH_WAVES - 1) / PH_WAVES;
+  const int grid = (int)(blocks > 16384 ? 16384 : blocks);
+  auto go = [&](auto zero) {
+    using T = decltype(zero);
+    if (dh == 64) k_heads_paged<T, 64><<<grid, PH_NT, 0, s>>>(a, (int)per, parts);
+    else k_heads_paged<T, 128><<<grid, PH_NT, 0, s>>>(a, (int)per, parts);
+  };
+  if (t == F32) go(float{});
+  else go(bf16_t{});
+}
+
+}  // namespace dy
