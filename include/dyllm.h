@@ -471,8 +471,8 @@ typedef struct {
 /* Attention of the rows over the keys and values of their requests' pages: row j is the query at position rows->pos[j].
  * q: [count, H, dh]; out: [count, H*dh]; kv_len: [R] tokens of each request whose keys are in place, the new ones among them (clamped to what
  * the table can hold).  scores: NULL for plain attention in both directions.  rows->slot is not looked at (may be NULL).  Table entries that name
- * no page of the pool are read as its first page, and set the status word to DYLLM_ERR_INVALID_ARG.  rows->cap <= the context's max_rows;
- * R <= DYLLM_MAX_REQUESTS.  Roundings as in dyllm_partial_attention_quant; kernel and key splits are chosen by rows->cap, R and
+ * no page of the pool are read as its first page, and set the status word to DYLLM_ERR_INVALID_ARG.  R <= DYLLM_MAX_REQUESTS; R and
+ * rows->cap may exceed the context's max_batch and max_rows (which the scratch for key splits goes by).  Roundings as in dyllm_partial_attention_quant; kernel and key splits are chosen by rows->cap, R and
  * max_pages on the host and by the lengths on the device. */
 int dyllm_paged_attention(dyllm_ctx *ctx, const void *q, const dyllm_pages *pages, const dyllm_page_rows *rows, int32_t R,
                           const int32_t *kv_len, const dyllm_scores *scores, void *out, void *stream);

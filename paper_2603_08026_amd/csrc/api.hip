@@ -45,6 +45,7 @@ struct dyllm_ctx {
   // projection, and k|v of the candidates of the approximate step (made ahead of another raw result)
   int32_t *plan, *plan_up, *plan_down, *plan_kv;
   int32_t *scan;   // words of the chained compaction kernel; all zero between calls
+  int32_t *arrive; // counters of attention's key splits (ARRIVE_WORDS); all zero between calls
   float *rope;     // [max_seq, dh/2, 2]
   uint64_t turns[64];  // what a pair of columns is turned by a position, in 2^-64 turns
   // optional per-stage timing (dyllm_profile_begin / _end)
@@ -57,7 +58,7 @@ struct dyllm_ctx {
 namespace {
 
 struct Layout {
-  size_t ns, qs, part_o, part_ml, cosb, flag, hs, fs, act, status, rope, dv_full, dc, csal, pos, win_idx, win_off, ksal, scan, total;
+  size_t ns, qs, part_o, part_ml, cosb, flag, hs, fs, act, status, rope, dv_full, dc, csal, pos, win_idx, win_off, ksal, scan, arrive, total;
   size_t part_elems, quant_part_elems;
 };
 
@@ -102,6 +103,7 @@ Layout make_layout(const dyllm_layer_cfg &c) {
   l.win_off = take(((size_t)c.max_batch + 1) * 4);
   l.ksal = take(R * dkv * e);
   l.scan = take((size_t)compact_scan_words() * 4);
+  l.arrive = take((size_t)ARRIVE_WORDS * 4);
   l.total = off;
   return l;
 }
@@ -690,7 +692,8 @@ ScoredAttn scored_args(const dyllm_ctx *ctx, const void *q, const dyllm_scores *
   a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.dh = c.head_dim;
   if (sc) { a.soft_cap = sc->cap; a.block = sc->block; a.prefix = sc->prefix; a.slopes = sc->slopes; a.doc = sc->doc; }
   a.part_o = ctx->part_o; a.part_ml = ctx->part_ml; a.part_elems = ctx->quant_part_elems;
-  a.n_split = (int32_t *)ctx->cosb;
+  a.arrive = ctx->arrive;
+  a.n_split = (int32_t *)ctx->cosb; a.split_rows = ctx->rows_cap;
   a.status = ctx->status; a.bad_page_code = DYLLM_ERR_INVALID_ARG;
   return a;
 }
@@ -755,6 +758,7 @@ int dyllm_create(const dyllm_layer_cfg *cfg, dyllm_ctx **out) {
   ctx->dv_full = b + l.dv_full; ctx->dc = b + l.dc; ctx->csal = b + l.csal; ctx->pos = (int32_t *)(b + l.pos);
   ctx->win_idx = (int32_t *)(b + l.win_idx); ctx->win_off = (int32_t *)(b + l.win_off);
   ctx->ksal = b + l.ksal; ctx->scan = (int32_t *)(b + l.scan);
+  ctx->arrive = (int32_t *)(b + l.arrive);
 
   // rotary table in double precision on the host, cleared status word
   const int half = cfg->head_dim / 2;
@@ -772,6 +776,7 @@ int dyllm_create(const dyllm_layer_cfg *cfg, dyllm_ctx **out) {
   if (e == hipSuccess) e = hipMemset(ctx->dv_full, 0, l.dc - l.dv_full);
   if (e == hipSuccess) e = hipMemset(ctx->pos, 0, l.win_idx - l.pos);
   if (e == hipSuccess) e = hipMemset(ctx->scan, 0, (size_t)compact_scan_words() * 4);
+  if (e == hipSuccess) e = hipMemset(ctx->arrive, 0, (size_t)ARRIVE_WORDS * 4);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     (void)hipFree(ctx->ws);
@@ -1299,7 +1304,6 @@ int dyllm_paged_attention(dyllm_ctx *ctx, const void *q, const dyllm_pages *page
   if ((rc = check_pages(ctx, pages, R, true, true))) return rc;
   if ((rc = check_page_rows(ctx, rows, true, false))) return rc;
   if ((rc = check_scores(ctx, scores, true))) return rc;
-  if (rows->cap > ctx->rows_cap) return fail(ctx, DYLLM_ERR_CAPACITY, "row capacity exceeds the context's max_rows");
   ScoredAttn a = scored_args(ctx, q, scores, out);
   a.pages = pages_of(pages);
   a.kv_len = kv_len; a.offsets = rows->offsets; a.at = rows->pos; a.cap = rows->cap;
@@ -1318,7 +1322,7 @@ int dyllm_partial_attention_masked(dyllm_ctx *ctx, const void *q_sal, const void
   if (!q_sal || !k_cache || !v_cache || !c_sal_out) return fail(ctx, DYLLM_ERR_INVALID_ARG, "NULL tensor");
   if (misaligned(q_sal) || misaligned(k_cache) || misaligned(v_cache) || misaligned(c_sal_out) || ((uintptr_t)kv_len & 3))
     return fail(ctx, DYLLM_ERR_INVALID_ARG, "misaligned tensor");
-  if ((rc = check_rows(ctx, rows, B, L, true, &r))) return rc;
+  if ((rc = check_rows(ctx, rows, B, L, false, &r))) return rc;
   if ((rc = check_scores(ctx, scores, false))) return rc;
   ScoredAttn a = scored_args(ctx, q_sal, scores, c_sal_out);
   a.k = k_cache; a.v = v_cache; a.kv_len = kv_len;

@@ -20,9 +20,13 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
-// scores as they are; reshaped (cap, slopes); documents too
-enum ScoreMode { PLAIN = 0, SHAPED = 1, DOCS = 2 };
-inline ScoreMode mode_of(const ScoredAttn &a) { return a.doc ? DOCS : a.soft_cap > 0.f || a.slopes ? SHAPED : PLAIN; }
+// What a kernel is made for, a bit each.  (Documents with cap or bias are one kernel, which asks for each of them as it goes; as branches of
+// one kernel cap and bias cost 8 to 25 %, since every branch copies the scores.)
+enum ScoreMode { PLAIN = 0, CAPPED = 1, BIASED = 2, DOCS = 4, DOCS_ANY = 7 };
+inline int mode_of(const ScoredAttn &a) {
+  const int shape = (a.soft_cap > 0.f ? CAPPED : 0) | (a.slopes ? BIASED : 0);
+  return !a.doc ? shape : shape ? DOCS_ANY : DOCS;
+}
 
 __device__ __forceinline__ int keys_of(const ScoredAttn &a, int b) { return a.kv_len ? min(max(a.kv_len[b], 0), a.L) : a.L; }
 
@@ -39,16 +43,16 @@ __device__ __forceinline__ int position_of(const ScoredAttn &a, bool pages, int 
 }
 
 // ---- work items: (key-value head, sequence, key split, tile of packed rows) ---------------------------------------
-// The rows of a sequence and the g heads of a group are packed as in the grouped form above.  Where rows are few the keys of a sequence are split so
-// that about `target` workgroups share all keys evenly, whatever the lengths (which the device knows): with W = sum of tiles * keys
-// over the sequences, a split has W * Hkv / target keys, and a sequence as many splits as that makes of its keys.
+// The rows of a sequence and the g heads of a group are packed as in the grouped form above.  Where rows are few the keys of a sequence are split, in
+// pieces of one size for all sequences, the smallest with which no more than a.target items are made: workgroups of ragged requests then
+// end together, and fit the chip in one round.  (The lengths are the device's to know.)
 constexpr int SPLIT_KEYS = 128;  // keys that the waves of a workgroup take at a time; a split has a multiple
 inline long scored_tiles(const ScoredAttn &a) {  // at most, of one key-value head
   const long g = a.H / a.Hkv;
   return a.offsets ? (a.cap * g + a.bq - 1) / a.bq + a.B : a.B * ((a.L * g + a.bq - 1) / a.bq);
 }
 inline long scored_items(const ScoredAttn &a) {
-  return scored_tiles(a) + (a.splits > 1 ? (a.target + a.Hkv - 1) / a.Hkv : 0);
+  return scored_tiles(a) + (a.splits > 1 ? (a.target + a.Hkv - 1) / a.Hkv : 0);  // (where the sizes of the pieces were not found: sum of ceilings)
 }
 // Which of the 8 XCDs takes which item: the tiles that read one (sequence, head)'s keys stay on as few as the heads allow, next to each other in time.
 inline long scored_grid(const ScoredAttn &a) {
@@ -60,6 +64,7 @@ inline long scored_grid(const ScoredAttn &a) {
 struct ScoredItem {
   int seq = -1, row = 0, packed = 0, n = 0;  // as AttnItem
   int kv_head = 0, keys = 0, split = 0, splits = 1, chunk = 0;
+  int counter = 0;  // number of the (tile, key-value head)
 };
 __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
   const int g = a.H / a.Hkv, lane = threadIdx.x % WAVE, BQ = a.bq;
@@ -77,25 +82,40 @@ __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
     }
   };
   int chunk = 0x7fffff80;
+  auto splits_of = [&](int *size) {
+    const int least = ((keys + a.splits - 1) / a.splits + SPLIT_KEYS - 1) / SPLIT_KEYS * SPLIT_KEYS;
+    *size = max(chunk, least);
+    return max(1, (int)(((long)keys + *size - 1) / *size));
+  };
   if (a.splits > 1) {
     float w = 0.f;
     for (int b0 = 0; b0 < a.B; b0 += WAVE) {
       look(b0);
       w += (float)tiles * (float)keys;
     }
-    w = wave_sum(w) * (float)a.Hkv / (float)a.target;  // (the order of additions is fixed: every workgroup has the same)
-    chunk = (int)fminf(w, 1e9f) / SPLIT_KEYS * SPLIT_KEYS + SPLIT_KEYS;
+    // (a first size from the sum, then what it makes of the sequences' ends; sums of whole numbers, and every workgroup finds the same)
+    float pieces = wave_sum(w) * (float)a.Hkv / (float)a.target;
+#pragma unroll 1
+    for (int round = 0; round < 4; ++round) {
+      chunk = max((int)ceilf(fminf(pieces, 1e9f) / SPLIT_KEYS), 1) * SPLIT_KEYS;
+      float items = 0.f;
+      for (int b0 = 0; b0 < a.B; b0 += WAVE) {
+        if (a.B > WAVE) look(b0);
+        int size;
+        items += (float)(tiles * splits_of(&size));
+      }
+      items = wave_sum(items) * (float)a.Hkv;
+      if (items <= (float)a.target) break;  // uniform
+      pieces = (float)chunk * fmaxf(items / (float)a.target, 1.02f);
+    }
   }
-  auto splits_of = [&](int *size) {
-    const int least = ((keys + a.splits - 1) / a.splits + SPLIT_KEYS - 1) / SPLIT_KEYS * SPLIT_KEYS;
-    *size = max(chunk, least);
-    return max(1, (int)(((long)keys + *size - 1) / *size));
-  };
-  int size = 0, upto = 0, n_items = 0;
+  int size = 0, upto = 0, tiles_to = 0, n_items = 0, n_tiles = 0;
   for (int b0 = 0; b0 < a.B; b0 += WAVE) {
     if (a.B > WAVE || a.splits == 1) look(b0);
     upto = wave_scan(tiles * splits_of(&size));
+    tiles_to = wave_scan(tiles);
     n_items += __builtin_amdgcn_readlane(upto, WAVE - 1);
+    n_tiles += __builtin_amdgcn_readlane(tiles_to, WAVE - 1);
   }
   const int x = p % ATTN_XCD, s = p / ATTN_XCD;
   int w;
@@ -116,10 +136,12 @@ __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
     it.kv_head = (int)(at / n_items);
     w = (int)(at % n_items);
   }
+  it.counter = it.kv_head * n_tiles;
   for (int b0 = 0; b0 < a.B; b0 += WAVE) {
     if (a.B > WAVE) {
       look(b0);
       upto = wave_scan(tiles * splits_of(&size));
+      tiles_to = wave_scan(tiles);
     }
     const uint64_t past = __ballot(upto > w);
     if (past) {
@@ -132,17 +154,125 @@ __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
       it.splits = max(1, (int)(((long)it.keys + it.chunk - 1) / it.chunk));
       const int mine = w - (__builtin_amdgcn_readlane(upto, f) - nt * it.splits);
       it.split = mine / nt;
-      it.packed = (nt - 1 - mine % nt) * BQ;  // the last rows of a causal sequence have the most keys: they come first
+      const int tile = nt - 1 - mine % nt;  // the last rows of a causal sequence have the most keys: they come first
+      it.counter += __builtin_amdgcn_readlane(tiles_to, f) - nt + tile;
+      it.packed = tile * BQ;
       it.n = min(BQ, rows * g - it.packed);
       return it;
     }
     w -= __builtin_amdgcn_readlane(upto, WAVE - 1);
+    it.counter += __builtin_amdgcn_readlane(tiles_to, WAVE - 1);
   }
   return it;
 }
 
+// ---- key splits: partial results, and their merge ------------------------------------------------------------------------
+// Few rows (a.fused): by the workgroup that arrives last.  Partial rows, their maxima (log2 units) and sums go past the caches of the die (device
+// scope), so that workgroups on other dies see them without a flush: stored, waited for, then counted.  The one that finds all others of its (tile,
+// head) counted merges, and leaves the counter at zero.  Many rows: by a launch of its own (k_scored_merge), which has the whole chip for them.
+// One token of one request of 32768 keys, 28 heads over 4: launch of its own / last one 44 / 28 us; of 8 requests of 8192, 8 over 2 of 64, 21.7 / 18.4; but 32 rows
+// of 16 x 1280 keys, 32 heads, 92 / 121.
+constexpr int MAX_SPLITS = 128;
+__device__ __forceinline__ void store_through(float *p, float2 v) {
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_through(const float *p) {
+  return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+// what a row's keys sum up to -> what its values are multiplied by (a row without keys: zero)
+__device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.0f / l; }
+
+// Called by all 256 threads, whose partial results are stored (not waited for); at most 8 rows.  flag: a word of LDS; buf: 4 * DH floats of it.
+// A row is taken by four waves, by two or by one, a wave takes up to two rows at a time: 16 splits of each are in flight.
+constexpr int FUSED_ROWS = 8;
+template <typename T, int DH> __device__ __forceinline__ void merge_splits_last(const ScoredAttn &a, const ScoredItem &item, int *flag, float *buf) {
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), grp = a.H / a.Hkv, splits = item.splits;
+  wait_vmcnt<0>();
+  __syncthreads();
+  if (tid == 0) {
+    const int before = __hip_atomic_fetch_add(a.arrive + item.counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before == splits - 1) __hip_atomic_store(a.arrive + item.counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = before == splits - 1;
+  }
+  __syncthreads();
+  if (!*flag) return;
+  constexpr int V = DH / WAVE, IN_FLIGHT = 16;
+  auto load = [&](const float *p, float (&x)[V]) {
+    if constexpr (V == 2) {
+      const float2 v = load_through(p);
+      x[0] = v.x; x[1] = v.y;
+    } else {
+      x[0] = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  };
+  const int parts = item.n == 1 ? 4 : item.n == 2 ? 2 : 1, first = wave / parts, part = wave % parts;  // waves of a row
+  if (first >= item.n) return;  // (only where a wave takes rows alone)
+  const size_t step = (size_t)a.cap * a.H;
+  const bool second = first + 4 < item.n;
+  size_t at[2];
+  float m[2][2], l[2][2], o[2][V], total[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int p = item.packed + (u && second ? first + 4 : first);
+    at[u] = (size_t)(item.row + p / grp) * a.H + item.kv_head * grp + p % grp;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int s = lane + h * WAVE;
+      const float2 ml = s < splits ? load_through(a.part_ml + (s * step + at[u]) * 2) : float2{-INFINITY, 0.f};
+      m[u][h] = ml.x; l[u][h] = ml.y;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[u][e] = 0.f;
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {  // m becomes the weights
+    const float M = wave_max(fmaxf(m[u][0], m[u][1])), ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) m[u][h] = __builtin_amdgcn_exp2f(m[u][h] - ref);
+    total[u] = wave_sum(l[u][0] * m[u][0] + l[u][1] * m[u][1]);
+  }
+  auto rows = [&](auto count_c) {
+    constexpr int N = decltype(count_c)::value;
+    for (int s0 = part; s0 < splits; s0 += IN_FLIGHT * parts) {  // (past the end the last split again, with no weight)
+      float x[N][IN_FLIGHT][V];
+#pragma unroll
+      for (int i = 0; i < IN_FLIGHT; ++i)
+#pragma unroll
+        for (int u = 0; u < N; ++u) load(a.part_o + (min(s0 + i * parts, splits - 1) * step + at[u]) * DH + lane * V, x[u][i]);
+#pragma unroll
+      for (int i = 0; i < IN_FLIGHT; ++i) {
+        const int s = s0 + i * parts;
+        if (s >= splits) break;  // uniform
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s < WAVE ? m[u][0] : m[u][1]), s % WAVE));
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[u][e] = fmaf(x[u][i][e], w, o[u][e]);
+        }
+      }
+    }
+  };
+  if (second) rows(std::integral_constant<int, 2>{});
+  else rows(std::integral_constant<int, 1>{});
+  if (parts > 1) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) buf[(wave * V + e) * WAVE + lane] = o[0][e];
+    __syncthreads();
+    if (part > 0) return;
+    for (int w = 1; w < parts; ++w)
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[0][e] += buf[((wave + w) * V + e) * WAVE + lane];
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    if (u && !second) break;
+    const float inv = inverse_of(total[u]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) ((T *)a.out)[at[u] * DH + lane * V + e] = from_f<T>(o[u][e] * inv);
+  }
+}
+
 // ---- shared pieces of the bf16 kernels -----------------------------------------------------------------------
-template <typename V> __device__ __forceinline__ void here(V &v) { asm volatile("" : "+v"(v)); }
 __device__ __forceinline__ const unsigned char *uniform_bytes(const void *p) {
   const uint64_t u = (uint64_t)p;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
@@ -216,69 +346,86 @@ template <int DH> struct KeyTile {
   __device__ static __forceinline__ int v_chunk(int r, int c) { return (v_pair(r, c >> 1) << 1) | (c & 1); }
 };
 
-// Documents of the rows: this row's, the least and the largest of the workgroup's, and where keys of that range start and end.
-// (One pass over the numbers of the sequence, 4 bytes a key, where the sweep reads 4 dh.)
-__device__ __forceinline__ void doc_range(const int32_t *doc, int n, int lo, int hi, int *red, int *first, int *end) {
-  int f = n, e = 0;
-  for (int j = threadIdx.x; j < n; j += blockDim.x) {
-    const int d = doc[j];
-    if (d >= lo && d <= hi) {
-      f = min(f, j);
-      e = max(e, j + 1);
+// Where keys of documents from lo to hi, those of a workgroup's rows, start and end, and whether all keys in between are of the one document that the rows
+// are of.  (One pass over the numbers of the sequence, 4 bytes a key, where the sweep reads 4 dh.)  red: 12 words of LDS.
+__device__ __forceinline__ void doc_range(const int32_t *doc, int n, int lo, int hi, int *red, int *first, int *end, bool *solid) {
+  int f = n, e = 0, count = 0;
+  constexpr int U = 8;  // numbers a thread has in flight
+  for (int j0 = threadIdx.x; j0 < n; j0 += 256 * U) {
+    int d[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) d[u] = doc[min(j0 + 256 * u, n - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + 256 * u;
+      if (j < n && d[u] >= lo && d[u] <= hi) {
+        f = min(f, j);
+        e = max(e, j + 1);
+        ++count;
+      }
     }
   }
   f = wave_min_i(f);
   e = wave_max_i(e);
-  const int w = threadIdx.x / WAVE, nw = blockDim.x / WAVE;
-  if (threadIdx.x % WAVE == 0) { red[2 * w] = f; red[2 * w + 1] = e; }
+  count = __builtin_amdgcn_readlane(wave_scan(count), WAVE - 1);
+  const int w = threadIdx.x / WAVE;
+  if (threadIdx.x % WAVE == 0) { red[3 * w] = f; red[3 * w + 1] = e; red[3 * w + 2] = count; }
   __syncthreads();
-  for (int i = 0; i < nw; ++i) { f = min(f, red[2 * i]); e = max(e, red[2 * i + 1]); }
+  count = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f = min(f, red[3 * i]);
+    e = max(e, red[3 * i + 1]);
+    count += red[3 * i + 2];
+  }
   *first = __builtin_amdgcn_readfirstlane(f);
   *end = __builtin_amdgcn_readfirstlane(e);
+  *solid = lo == hi && __builtin_amdgcn_readfirstlane(count) == *end - *first;
 }
 
 // A row's part in the masks and the scores' shape.
 struct RowMask {
   int limit = 0, doc = -1;
-  float pos = 0.f, slope = 0.f;  // slope in log2 units
+  float pos = 0.f, slope = 0.f;  // slope in units of the score as it goes into the exponential's multiply-add
 };
 
-// x = q.k (not scaled) -> log2 units, reshaped
+// x = q.k (not scaled) -> reshaped; x * sc is in log2 units (a capped one is so itself: sc = 1)
 struct Shape {
-  float sc, cap_in, cap_out;  // scale to log2 units; 2 log2e / (sqrt(dh) cap), cap log2e
+  float sc, cap_in, cap_out;  // cap_in = 2 log2e / (sqrt(dh) cap), cap_out = cap log2e
   bool capped, sloped;
   __device__ __forceinline__ Shape(const ScoredAttn &a) {
     const float scale = 1.0f / sqrtf((float)a.dh);
-    sc = scale * LOG2E;
     capped = a.soft_cap > 0.f;
     sloped = a.slopes != nullptr;
+    sc = capped ? 1.f : scale * LOG2E;
     cap_in = capped ? 2.0f * LOG2E * scale / a.soft_cap : 0.f;
     cap_out = a.soft_cap * LOG2E;
   }
+  __device__ __forceinline__ float slope(float x) const { return x * LOG2E / sc; }
   // c tanh(y) = c - 2c / (1 + e^2y): an exponential and a reciprocal; both ends are right (e^2y = 0 and infinity)
   __device__ __forceinline__ float cap(float x) const {
     return fmaf(-2.0f * cap_out, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * cap_in)), cap_out);
   }
 };
 
-__device__ __forceinline__ uint32_t any_nonfinite(const uint4 &w) {  // bits 15 and 31: exponents that are all ones
-  uint32_t r = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r |= ((&w.x)[i] & 0x7f807f80u) + 0x00800080u;
-  return r;
-}
-
 // Values that are no finite numbers, in a tile where some keys count for some rows only.  A matrix product gives 0 * inf = NaN to rows that the key does
 // not count for.  So these values are taken out, and what they do to rows with a weight for them is found by products with 0 and 1 (is it NaN,
-// +inf, -inf) in place of the values.  Rare: no cost beyond the look at the exponents in tiles that are tested key by key.
+// +inf, -inf) in place of the values.  Rare: no cost beyond the look at the values of tiles that are tested key by key.
 template <int DB>
 __device__ __forceinline__ void take_out_nonfinite(bf16x8 (&vf)[2][DB], const bf16x8 (&pf)[2], floatx16 (&acc)[DB]) {
-  uint32_t any = 0;
+  float none = 0.f;  // 0 times a number is 0, times anything else NaN: two values an instruction
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) any |= any_nonfinite(__builtin_bit_cast(uint4, vf[k][db]));
-  if (!__any(any & 0x80008000u)) return;
+    for (int db = 0; db < DB; ++db) {
+      const uint4 w = __builtin_bit_cast(uint4, vf[k][db]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t u = (&w.x)[i];
+        none = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, u), __builtin_bit_cast(bf16x2_t, 0u), none, false);
+      }
+    }
+  if (!__any(none != 0.f)) return;
 #pragma unroll 1
   for (int kind = 0; kind < 3; ++kind) {
     const uint32_t mask = kind == 0 ? 0x7fffu : 0xffffu, base = kind == 0 ? 0x7f81u : kind == 1 ? 0x7f80u : 0xff80u, span = kind == 0 ? 0x7fu : 1u;
@@ -318,29 +465,41 @@ __device__ __forceinline__ void take_out_nonfinite(bf16x8 (&vf)[2][DB], const bf
     }
 }
 
-// Scores of a lane's 16 keys of the tile at k0 -> log2 units (SHAPED, DOCS); keys that do not count -> -inf.  Returns whether any test was
-// needed (uniform).  least: the least limit of the wave's rows.  docs: the tile's 32 numbers in LDS; one: the wave's rows are of one document.
+// What a tile's keys have to be tested for.
+struct TileTests {
+  int least = 0;       // limits of the wave's rows: the least
+  int first = 0;       // documents: keys below do not count
+  bool one = true;     // ... the wave's rows are of one
+  bool solid = false;  // ... and so are all keys from `first` to the largest limit
+};
+// Scores of a lane's 16 keys of the tile at k0, reshaped; keys that do not count -> -inf.  Returns whether any was tested (uniform).  docs: the tile's
+// 32 numbers in LDS.
 template <int MODE>
-__device__ __forceinline__ bool shape_scores(floatx16 &s, const Shape &sh, const RowMask &row, int k0, int lhi, int l32, int least, const int32_t *docs, bool one) {
+__device__ __forceinline__ bool shape_scores(floatx16 &s, const Shape &sh, const RowMask &row, const TileTests &t, int k0, int lhi, int l32, const int32_t *docs) {
   const int key0 = k0 + 4 * lhi;
-  if constexpr (MODE != PLAIN) {
-    if (sh.capped) {
+  if constexpr (MODE & CAPPED) {
+    if (MODE != DOCS_ANY || sh.capped) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = sh.cap(s[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] *= sh.sc;
     }
-    if (sh.sloped) {
+  }
+  if constexpr (MODE & BIASED) {
+    if (MODE != DOCS_ANY || sh.sloped) {
       const float d0 = row.pos - (float)key0;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = fmaf(-row.slope, fabsf(d0 - (float)(8 * (e / 4) + (e % 4))), s[e]);
     }
   }
   bool tested = false;
-  if constexpr (MODE == DOCS) {
-    const uint32_t same = (uint32_t)__ballot(docs[l32] == row.doc);
-    if (!one) {
+  if constexpr (MODE & DOCS) {
+    if (t.solid) {
+      if (k0 < t.first) {  // uniform
+        tested = true;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (key0 + 8 * (e / 4) + (e % 4) < t.first) s[e] = -INFINITY;
+      }
+    } else if (!t.one) {
       tested = true;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -350,14 +509,14 @@ __device__ __forceinline__ bool shape_scores(floatx16 &s, const Shape &sh, const
         s[4 * g + 2] = d.z == row.doc ? s[4 * g + 2] : -INFINITY;
         s[4 * g + 3] = d.w == row.doc ? s[4 * g + 3] : -INFINITY;
       }
-    } else if (same != 0xffffffffu) {
+    } else if (const uint32_t same = (uint32_t)__ballot(docs[l32] == row.doc); same != 0xffffffffu) {
       tested = true;
       const uint32_t mine = same >> (4 * lhi);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = (mine >> (8 * (e / 4) + (e % 4))) & 1u ? s[e] : -INFINITY;
     }
   }
-  if (k0 + 32 > least) {  // uniform
+  if (k0 + 32 > t.least) {  // uniform
     tested = true;
 #pragma unroll
     for (int e = 0; e < 16; ++e)
@@ -368,9 +527,17 @@ __device__ __forceinline__ bool shape_scores(floatx16 &s, const Shape &sh, const
 
 // un-normalised rows of a split.  (A split without a key for the row: maximum -inf, sum 0.)
 template <int DH>
-__device__ __forceinline__ void store_scored_partial(const ScoredAttn &a, const floatx16 (&acc_o)[DH / 32], int split, uint32_t place, int lhi, float m_run, float l_run) {
-  const size_t at = (size_t)split * a.cap * a.H + place;
+__device__ __forceinline__ void store_scored_partial(const ScoredAttn &a, const floatx16 (&acc_o)[DH / 32], const ScoredItem &item, uint32_t place, int jq, int lhi, float m_run, float l_run) {
+  const size_t at = (size_t)item.split * a.cap * a.H + place;
   float *po = a.part_o + at * DH + 4 * lhi;
+  if (a.fused) {
+#pragma unroll
+    for (int db = 0; db < DH / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 8; ++g) store_through(po + db * 32 + 8 * (g / 2) + 2 * (g % 2), float2{acc_o[db][2 * g], acc_o[db][2 * g + 1]});
+    if (lhi == 0) store_through(a.part_ml + at * 2, float2{m_run, l_run});
+    return;
+  }
 #pragma unroll
   for (int db = 0; db < DH / 32; ++db)
 #pragma unroll
@@ -379,13 +546,12 @@ __device__ __forceinline__ void store_scored_partial(const ScoredAttn &a, const 
   if (lhi == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = float2{m_run, l_run};
 }
 
-// what a row's keys sum up to -> what its values are multiplied by (a row without keys: zero)
-__device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.0f / l; }
-
+// (a.once: keys and values past the L2)
 void launch_scored_pages_few(const ScoredAttn &a, hipStream_t s);
 void launch_scored_pages_many(const ScoredAttn &a, hipStream_t s);
+void launch_scored_pages_once(const ScoredAttn &a, hipStream_t s);
 void launch_scored_dense_few(const ScoredAttn &a, hipStream_t s);
 void launch_scored_dense_many(const ScoredAttn &a, hipStream_t s);
-void launch_scored_f32(const ScoredAttn &a, hipStream_t s);
+void launch_scored_dense_once(const ScoredAttn &a, hipStream_t s);
 
 }  // namespace dy

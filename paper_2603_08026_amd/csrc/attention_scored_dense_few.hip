@@ -2,5 +2,5 @@
 #include "attention_scored_kernels.h"
 
 namespace dy {
-void launch_scored_dense_few(const ScoredAttn &a, hipStream_t s) { launch_by_shape<false, false>(a, s); }
+void launch_scored_dense_few(const ScoredAttn &a, hipStream_t s) { launch_by_shape<Form::FEW, false>(a, s); }
 }  // namespace dy

@@ -2,5 +2,5 @@
 #include "attention_scored_kernels.h"
 
 namespace dy {
-void launch_scored_dense_many(const ScoredAttn &a, hipStream_t s) { launch_by_shape<true, false>(a, s); }
+void launch_scored_dense_many(const ScoredAttn &a, hipStream_t s) { launch_by_shape<Form::MANY, false>(a, s); }
 }  // namespace dy

@@ -14,7 +14,7 @@ namespace {
 template <int DH, int MODE> struct FewTile : KeyTile<DH> {
   using K = KeyTile<DH>;
   static constexpr int NW = 4, NS = 2, BQ = 32;
-  static constexpr int STAGE = 2 * K::REGION + (MODE == DOCS ? 256 : 0), PER_TILE = 2 * K::COPIES + (MODE == DOCS);
+  static constexpr int STAGE = 2 * K::REGION + (MODE & DOCS ? 256 : 0), PER_TILE = 2 * K::COPIES + (MODE & DOCS ? 1 : 0);
   static constexpr int PER_WAVE = (K::DB * 16 + 2) * 64;  // floats of a wave's result
   static constexpr int RING = NS * STAGE, LDS = NW * RING;
   static_assert((NS - 1) * PER_TILE < 64 && (NW - 1) * PER_WAVE * 4 <= LDS && LDS <= 160 * 1024, "vmcnt immediate, merge scratch");
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
   using T = FewTile<DH, MODE>;
   constexpr int TK = T::TK, ROWB = T::ROWB, DB = T::DB, KK = T::KK, CH = T::CH, RPC = T::RPC, NW = T::NW, NS = T::NS, COPIES = T::COPIES;
   __shared__ __align__(1024) unsigned char smem[T::LDS];
-  __shared__ int red[2 * NW];
+  __shared__ int red[3 * NW];
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int l32 = lane % 32, lhi = lane / 32;
   const ScoredItem item = scored_item(a, blockIdx.x);
@@ -35,28 +35,28 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
   // this lane's query (rows past the end: the last one again, their results are never stored)
   const int p = item.packed + min(l32, nq - 1), jq = item.row + p / grp, hq = kvh * grp + p % grp;
   const uint32_t place = (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq;
+  const Shape sh(a);
   RowMask row;
-  bool one = true;
+  TileTests tests;
   int k_lo = split * item.chunk, k_hi;
   {
     const int i = position_of(a, PAGED, b, jq);
     row.limit = limit_of(a, b, item.keys, i);
     row.pos = (float)i;
-    if (MODE != PLAIN && a.slopes) row.slope = a.slopes[hq] * LOG2E;
-    int doc_first = 0;
-    if constexpr (MODE == DOCS) {
+    if ((MODE & BIASED) && a.slopes) row.slope = sh.slope(a.slopes[hq]);
+    if constexpr (MODE & DOCS) {
       row.doc = i >= 0 && i < a.L ? a.doc[(size_t)b * a.L + i] : -1;
       if (row.doc < 0) row.limit = 0;
       const int some = row.doc < 0 ? 0x7fffffff : row.doc, lo = wave_min_i(some), hi = wave_max_i(row.doc);
-      one = __all(row.doc == hi);
+      tests.one = __all(row.doc == hi);
       int end;
-      doc_range(a.doc + (size_t)b * a.L, item.keys, lo, hi, red, &doc_first, &end);
+      doc_range(a.doc + (size_t)b * a.L, item.keys, lo, hi, red, &tests.first, &end, &tests.solid);
       row.limit = min(row.limit, end);  // (the sweep ends there, in the middle of a tile)
     }
     k_hi = min(wave_max_i(row.limit), (int)min((long)k_lo + item.chunk, 0x7fffffffl));
-    if (MODE == DOCS) k_lo = max(k_lo, doc_first / TK * TK);
+    if (MODE & DOCS) k_lo = max(k_lo, tests.first / TK * TK);
+    tests.least = wave_min_i(row.limit);
   }
-  const int least = wave_min_i(row.limit);
   const int tiles = k_hi > k_lo ? (k_hi - k_lo + TK - 1) / TK : 0, n_tiles = tiles > wave ? (tiles - wave + NW - 1) / NW : 0;  // this wave's: wave, wave + 4, ..
 
   unsigned char *own = smem + wave * T::RING;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
         dma16(places.v + o + T::v_chunk(to, lane % CH) * 16, base + T::REGION + i * 1024u);
       }
     }
-    if constexpr (MODE == DOCS) dma4(a.doc + (size_t)b * a.L + k0 + min(l32, last), base + 2 * T::REGION);
+    if constexpr (MODE & DOCS) dma4(a.doc + (size_t)b * a.L + k0 + min(l32, last), base + 2 * T::REGION);
   };
 #pragma unroll
   for (int s = 0; s < NS; ++s)
@@ -111,8 +111,7 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc_o[db][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  const Shape sh(a);
-  const float sc = MODE == PLAIN ? sh.sc : 1.f;  // scores are kept in the log2 domain
+  const float sc = sh.sc;
   const int vrow = 4 * lhi + (lane % 16) / 4, hb = (lane / 16) & 1;
 
   for (int n = 0; n < n_tiles; ++n) {
@@ -137,7 +136,7 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
         const shortx4 g1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4 *)(at + 8 * ROWB));
         vf[ks][db] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7));
       }
-    const bool tested = shape_scores<MODE>(s, sh, row, key_of(n), lhi, l32, least, reinterpret_cast<const int32_t *>(st + 2 * T::REGION), one);
+    const bool tested = shape_scores<MODE>(s, sh, row, tests, key_of(n), lhi, l32, reinterpret_cast<const int32_t *>(st + 2 * T::REGION));
     float mx = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
@@ -190,41 +189,43 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
     dst[(DB * 16 + 1) * 64] = l_run;
   }
   __syncthreads();
-  if (wave > 0) return;
-  float M = m_run;
+  if (wave > 0 && (item.splits == 1 || !a.fused)) return;
+  if (wave == 0) {
+    float M = m_run;
 #pragma unroll
-  for (int w = 1; w < NW; ++w) M = fmaxf(M, mg[(size_t)(w - 1) * T::PER_WAVE + (DB * 16) * 64 + lane]);
-  const float ref = (M == -INFINITY) ? 0.f : M;
-  const float c0 = __builtin_amdgcn_exp2f(m_run - ref);
-  l_run *= c0;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc_o[db][e] *= c0;
-#pragma unroll
-  for (int w = 1; w < NW; ++w) {
-    const float *src = mg + (size_t)(w - 1) * T::PER_WAVE + lane;
-    const float cw = __builtin_amdgcn_exp2f(src[(DB * 16) * 64] - ref);
-    l_run = fmaf(src[(DB * 16 + 1) * 64], cw, l_run);
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, mg[(size_t)(w - 1) * T::PER_WAVE + (DB * 16) * 64 + lane]);
+    const float ref = (M == -INFINITY) ? 0.f : M;
+    const float c0 = __builtin_amdgcn_exp2f(m_run - ref);
+    l_run *= c0;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc_o[db][e] = fmaf(src[(db * 16 + e) * 64], cw, acc_o[db][e]);
-  }
-  if (l32 >= nq) return;
-  if (a.splits > 1 && kvh == 0 && split == 0 && lhi == 0) a.n_split[jq] = item.splits;
-  if (item.splits > 1) {
-    store_scored_partial<DH>(a, acc_o, split, place, lhi, M, l_run);
-    return;
-  }
-  const float inv = inverse_of(l_run);
-  bf16_t *out = (bf16_t *)a.out + (size_t)place * DH + 4 * lhi;
+      for (int e = 0; e < 16; ++e) acc_o[db][e] *= c0;
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
+    for (int w = 1; w < NW; ++w) {
+      const float *src = mg + (size_t)(w - 1) * T::PER_WAVE + lane;
+      const float cw = __builtin_amdgcn_exp2f(src[(DB * 16) * 64] - ref);
+      l_run = fmaf(src[(DB * 16 + 1) * 64], cw, l_run);
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<uint2 *>(out + db * 32 + 8 * g) =
-          uint2{pack_bf16(acc_o[db][4 * g] * inv, acc_o[db][4 * g + 1] * inv), pack_bf16(acc_o[db][4 * g + 2] * inv, acc_o[db][4 * g + 3] * inv)};
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc_o[db][e] = fmaf(src[(db * 16 + e) * 64], cw, acc_o[db][e]);
+    }
+    if (a.n_split && kvh == 0 && split == 0 && lhi == 0 && l32 < nq) a.n_split[jq] = item.splits;
+    if (item.splits > 1) {
+      if (l32 < nq) store_scored_partial<DH>(a, acc_o, item, place, jq, lhi, M, l_run);
+    } else if (l32 < nq) {
+      const float inv = inverse_of(l_run);
+      bf16_t *out = (bf16_t *)a.out + (size_t)place * DH + 4 * lhi;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<uint2 *>(out + db * 32 + 8 * g) =
+              uint2{pack_bf16(acc_o[db][4 * g] * inv, acc_o[db][4 * g + 1] * inv), pack_bf16(acc_o[db][4 * g + 2] * inv, acc_o[db][4 * g + 3] * inv)};
+    }
+  }
+  if (item.splits > 1 && a.fused) merge_splits_last<bf16_t, DH>(a, item, red, mg);
 }
 
 // ---- 128 packed rows a workgroup: many rows ----------------------------------------------------------------------
@@ -235,18 +236,19 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
 template <int DH, int MODE> struct ManyTile : KeyTile<DH> {
   using K = KeyTile<DH>;
   static constexpr int NW = 4, NS = 4, BQ = 128;
-  static constexpr int STAGE = 2 * K::REGION + (MODE == DOCS ? NW * 256 : 0);
-  static constexpr int CPW = K::COPIES / NW, LPW = 2 * CPW + (MODE == DOCS);  // copies a wave and tile
+  static constexpr int STAGE = 2 * K::REGION + (MODE & DOCS ? NW * 256 : 0);
+  static constexpr int CPW = K::COPIES / NW, LPW = 2 * CPW + (MODE & DOCS ? 1 : 0);  // copies a wave and tile
   static constexpr int SLOTS = K::DB + K::KK, LDS = NS * STAGE;
   static_assert(CPW >= 1 && (NS - 2) * LPW < 64 && LDS <= 80 * 1024 && BQ * K::ROWB <= LDS, "two workgroups a CU; rows leave by way of the same memory");
 };
 
-template <int DH, bool PAGED, int MODE>
+// ONCE: keys and values are copied past the L2.
+template <int DH, bool PAGED, int MODE, bool ONCE>
 __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   using T = ManyTile<DH, MODE>;
   constexpr int TK = T::TK, ROWB = T::ROWB, DB = T::DB, KK = T::KK, CH = T::CH, RPC = T::RPC, NW = T::NW, NS = T::NS, CPW = T::CPW, LPW = T::LPW, SLOTS = T::SLOTS;
   __shared__ __align__(1024) unsigned char smem[T::LDS];
-  __shared__ int red[2 * NW], red2[3 * NW];
+  __shared__ int red[3 * NW], red2[3 * NW];
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int l32 = lane % 32, lhi = lane / 32;
   const ScoredItem item = scored_item(a, blockIdx.x);
@@ -255,21 +257,22 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   const int nq = item.n, grp = a.H / a.Hkv;
   const int p = item.packed + min(wave * 32 + l32, nq - 1), jq = item.row + p / grp, hq = kvh * grp + p % grp;
   const uint32_t place = (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq;
+  const Shape sh(a);
   RowMask row;
-  bool one = true;
-  int k_lo = split * item.chunk, k_hi, least, most;  // least, most: limits of this wave's rows
+  TileTests tests;
+  int k_lo = split * item.chunk, k_hi, most;  // most: the largest limit of this wave's rows
   {
     const int i = position_of(a, PAGED, b, jq);
     row.limit = limit_of(a, b, item.keys, i);
     row.pos = (float)i;
-    if (MODE != PLAIN && a.slopes) row.slope = a.slopes[hq] * LOG2E;
+    if ((MODE & BIASED) && a.slopes) row.slope = sh.slope(a.slopes[hq]);
     int lo = 0x7fffffff, hi = -1;
-    if constexpr (MODE == DOCS) {
+    if constexpr (MODE & DOCS) {
       row.doc = i >= 0 && i < a.L ? a.doc[(size_t)b * a.L + i] : -1;
       if (row.doc < 0) row.limit = 0;
       lo = wave_min_i(row.doc < 0 ? 0x7fffffff : row.doc);
       hi = wave_max_i(row.doc);
-      one = __all(row.doc == hi);
+      tests.one = __all(row.doc == hi);
     }
     most = wave_max_i(row.limit);
     if (lane == 0) { red2[3 * wave] = most; red2[3 * wave + 1] = lo; red2[3 * wave + 2] = hi; }
@@ -282,21 +285,21 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       hi = max(hi, red2[3 * w + 2]);
     }
     all = __builtin_amdgcn_readfirstlane(all);
-    if constexpr (MODE == DOCS) {
-      int first, end;
-      doc_range(a.doc + (size_t)b * a.L, item.keys, lo, hi, red, &first, &end);
+    if constexpr (MODE & DOCS) {
+      int end;
+      doc_range(a.doc + (size_t)b * a.L, item.keys, lo, hi, red, &tests.first, &end, &tests.solid);
       row.limit = min(row.limit, end);  // (the sweep ends there, in the middle of a tile)
       all = min(all, end);
-      k_lo = max(k_lo, first / TK * TK);
+      k_lo = max(k_lo, tests.first / TK * TK);
     }
-    least = wave_min_i(row.limit);
+    tests.least = wave_min_i(row.limit);
     k_hi = min(all, (int)min((long)split * item.chunk + item.chunk, 0x7fffffffl));
     k_hi = max(k_hi, k_lo);
   }
   const int n_tiles = (k_hi - k_lo + TK - 1) / TK;
   // this wave's tiles: up to its rows' largest limit (rows that do not exist: none), the first n_clean of them without tests
   const int n_mine = wave * 32 >= nq ? 0 : min(n_tiles, max(0, (min(most, k_hi) - k_lo + TK - 1) / TK));
-  const int n_clean = MODE == DOCS ? 0 : max(0, (least - k_lo) / TK);
+  const int n_clean = (MODE & DOCS) && !tests.solid ? 0 : max(0, (tests.least - k_lo) / TK);
 
   bf16x8 qf[KK];
 #pragma unroll
@@ -307,8 +310,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc_o[db][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  const Shape sh(a);
-  const float sc = MODE == PLAIN ? sh.sc : 1.f;  // scores are kept in the log2 domain
+  const float sc = sh.sc;
 
   // Copies: copy c of a wave fills rows (c * NW + wave) * RPC and on.
   const uint32_t lds0 = lds_offset_of(smem);
@@ -320,14 +322,15 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   size_t off[2];
   auto one_copy = [&](int t, int c) {  // of a tile all of whose keys exist
     const uint32_t base = lds0 + (uint32_t)(t % NS) * T::STAGE;
-    if (MODE == DOCS && c == 2 * CPW) {
+    if ((MODE & DOCS) && c == 2 * CPW) {
       dma4(a.doc + (size_t)b * a.L + k_lo + t * TK + l32, base + 2 * T::REGION + wave * 256u);
       return;
     }
     const int i = c / 2;
     const size_t o = off[CPW == 1 ? wave * RPC / 16 : i];
     const uint32_t to = __builtin_amdgcn_readfirstlane(base + (c & 1) * T::REGION + (uint32_t)(i * NW + wave) * 1024u);
-    dma16_s((c & 1 ? places.v : places.k) + o, c & 1 ? off_v : off_k, to);
+    if constexpr (ONCE) dma16_s_once((c & 1 ? places.v : places.k) + o, c & 1 ? off_v : off_k, to);
+    else dma16_s((c & 1 ? places.v : places.k) + o, c & 1 ? off_v : off_k, to);
   };
   auto last_copies = [&](int t) {  // keys past the end are the last one again, masked later
     const uint32_t base = lds0 + (uint32_t)(t % NS) * T::STAGE;
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       dma16(places.k + o + T::k_chunk(to, lane % CH) * 16, base + (uint32_t)(i * NW + wave) * 1024u);
       dma16(places.v + o + T::v_chunk(to, lane % CH) * 16, base + T::REGION + (uint32_t)(i * NW + wave) * 1024u);
     }
-    if (MODE == DOCS) dma4(a.doc + (size_t)b * a.L + k_lo + t * TK + min(l32, last), base + 2 * T::REGION + wave * 256u);
+    if (MODE & DOCS) dma4(a.doc + (size_t)b * a.L + k_lo + t * TK + min(l32, last), base + 2 * T::REGION + wave * 256u);
   };
   auto full = [&](int t) { return k_lo + (t + 1) * TK <= k_hi; };
   auto next_halves = [&](int t) {  // where tile t lies, and the question for the one behind it
@@ -390,9 +393,12 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
     }
     const int vrow = 4 * lhi + (lane % 16) / 4, hb = (lane / 16) & 1;
     auto pv = [&](int ks, int db) { acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks][db], pf[ks], acc_o[db], 0, 0, 0); };
-    // CLEAN: tile t needs no test and tile t + NS - 1 exists in full.  STAGE: the LDS stage of tile t where it is known when compiled, else -1.
-    auto body = [&](int t, auto clean_c, auto stage_c) {
-      constexpr bool CLEAN = decltype(clean_c)::value;
+    // TEST: what tile t is tested for: NOTHING (then tile t + NS - 1 exists in full), the rows' LIMITs, or ALL.  STAGE: the LDS stage of tile t where
+    // it is known when compiled, else -1.
+    enum { NOTHING, LIMIT, ALL };
+    auto body = [&](int t, auto test_c, auto stage_c) {
+      constexpr int TEST = decltype(test_c)::value;
+      constexpr bool CLEAN = TEST == NOTHING;
       constexpr int STAGE = decltype(stage_c)::value;
       const int sidx = STAGE >= 0 ? STAGE : t % NS;
       const bool more = CLEAN || t + NS - 1 < n_tiles, spread = CLEAN || (more && full(t + NS - 1));
@@ -404,7 +410,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       auto copy_behind = [&](int product) {
         constexpr int EVERY = (DB + SLOTS) / (2 * CPW);
         if (product % EVERY == EVERY / 2 && (CLEAN || spread)) one_copy(t + NS - 1, product / EVERY);
-        if (MODE == DOCS && product == DB + SLOTS - 1 && spread) one_copy(t + NS - 1, 2 * CPW);
+        if ((MODE & DOCS) && product == DB + SLOTS - 1 && spread) one_copy(t + NS - 1, 2 * CPW);
       };
       const unsigned char *st = smem + (size_t)sidx * T::STAGE;
       const unsigned char *st_next = smem + (size_t)((sidx + 1) % NS) * T::STAGE;
@@ -418,19 +424,31 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       };
 #pragma unroll
       for (int kk = 0; kk < KK / 2; ++kk) read_k(kk);
-      bool tested = false;
-      if (!CLEAN || MODE != PLAIN)
-        tested = shape_scores<MODE>(s_cur, sh, row, k_lo + t * TK, lhi, l32, CLEAN ? 0x7fffffff : least,
-                                    reinterpret_cast<const int32_t *>(st + 2 * T::REGION + wave * 256), one);
+      // Reshaping and the test of limits: behind the first products, without a branch; other tests ahead of everything.
+      const int k0 = k_lo + t * TK, below = row.limit - (k0 + 4 * lhi);
+      const float d0 = row.pos - (float)(k0 + 4 * lhi);
+      bool tested = TEST == LIMIT;
+      if constexpr (TEST == ALL)
+        tested = shape_scores<MODE>(s_cur, sh, row, tests, k0, lhi, l32, reinterpret_cast<const int32_t *>(st + 2 * T::REGION + wave * 256));
       __builtin_amdgcn_sched_barrier(0);
-      float mx = s_cur[0];
+      float mx = -INFINITY;
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         pv(0, db);
         read_k(KK / 2 + db);
         copy_behind(db);
+        constexpr int PER = 16 / DB;
+        if constexpr (TEST != ALL) {
 #pragma unroll
-        for (int e = 16 / DB * db; e < 16 / DB * (db + 1); ++e) mx = fmaxf(mx, s_cur[e]);
+          for (int e = PER * db; e < PER * (db + 1); ++e) {
+            const int key = 8 * (e / 4) + (e % 4);
+            if (MODE & CAPPED) s_cur[e] = sh.cap(s_cur[e]);
+            if (MODE & BIASED) s_cur[e] = fmaf(-row.slope, fabsf(d0 - (float)key), s_cur[e]);
+            if (TEST == LIMIT) s_cur[e] = key < below ? s_cur[e] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int e = PER * db; e < PER * (db + 1); ++e) mx = fmaxf(mx, s_cur[e]);
         __builtin_amdgcn_sched_barrier(0);
       }
       mx = xhalf_max(mx) * sc;
@@ -486,21 +504,30 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       l_run += ps0 + ps1;  // (this lane's keys; the other half's are added behind the loop)
       pf[0] = __builtin_bit_cast(bf16x8, uint4{pw[0], pw[1], pw[2], pw[3]});
       pf[1] = __builtin_bit_cast(bf16x8, uint4{pw[4], pw[5], pw[6], pw[7]});
-      if (!CLEAN && tested) take_out_nonfinite<DB>(vf, pf, acc_o);
+      if (tested) take_out_nonfinite<DB>(vf, pf, acc_o);
       s_cur = s_next;
     };
-    int t = 0;
     const int n_fast = min(min(n_clean, n_mine), n_tiles - NS);  // (each with a further tile to fetch that is not the last)
-    using dyn = std::integral_constant<int, -1>;
-    if constexpr (MODE != DOCS) {
-      for (; t + NS <= n_fast; t += NS) {  // t % NS == 0 here
-        body(t, std::true_type{}, std::integral_constant<int, 0>{});
-        body(t + 1, std::true_type{}, std::integral_constant<int, 1>{});
-        body(t + 2, std::true_type{}, std::integral_constant<int, 2>{});
-        body(t + 3, std::true_type{}, std::integral_constant<int, 3>{});
+    auto one = [&](int t, auto test_c) { body(t, test_c, std::integral_constant<int, -1>{}); };
+    using nothing = std::integral_constant<int, NOTHING>;
+    using limit = std::integral_constant<int, LIMIT>;
+    using all = std::integral_constant<int, ALL>;
+    int t = 0;
+    if constexpr (MODE == DOCS_ANY) {
+      for (; t < n_mine; ++t) one(t, all{});
+    } else {
+      if constexpr (MODE == DOCS) {
+        const int n_all = tests.solid ? (tests.first > k_lo ? min(NS, n_mine) : 0) : n_mine;  // (solid: the first tile may have keys of another document)
+        for (; t < n_all; ++t) one(t, all{});
       }
+      for (; t + NS <= n_fast; t += NS) {  // t % NS == 0 here
+        body(t, nothing{}, std::integral_constant<int, 0>{});
+        body(t + 1, nothing{}, std::integral_constant<int, 1>{});
+        body(t + 2, nothing{}, std::integral_constant<int, 2>{});
+        body(t + 3, nothing{}, std::integral_constant<int, 3>{});
+      }
+      for (; t < n_mine; ++t) one(t, limit{});
     }
-    for (; t < n_mine; ++t) body(t, std::false_type{}, dyn{});
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -515,13 +542,14 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   }
   if (PAGED && places.bad && lane == 0) *a.status = a.bad_page_code;
   __syncthreads();  // every wave is done with the tiles
-  if (wave * 32 >= nq) return;
   const bool exists = wave * 32 + l32 < nq;
-  if (a.splits > 1 && kvh == 0 && split == 0 && lhi == 0 && exists) a.n_split[jq] = item.splits;
+  if (a.n_split && kvh == 0 && split == 0 && lhi == 0 && exists) a.n_split[jq] = item.splits;
   if (item.splits > 1) {
-    if (exists) store_scored_partial<DH>(a, acc_o, split, place, lhi, m_run, l_run);
+    if (exists) store_scored_partial<DH>(a, acc_o, item, place, jq, lhi, m_run, l_run);
+    if (a.fused) merge_splits_last<bf16_t, DH>(a, item, red, reinterpret_cast<float *>(smem));
     return;
   }
+  if (wave * 32 >= nq) return;
   // whole rows leave by way of LDS: 16-byte chunk c of row r lies at c ^ (r % chunks)
   constexpr int RPI = WAVE / CH;
   unsigned char *rows = smem + wave * 32 * ROWB;
@@ -543,22 +571,26 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   }
 }
 
-template <bool MANY, int DH, bool PAGED, int MODE> void launch_scored(const ScoredAttn &a, hipStream_t s) {
-  if constexpr (MANY) k_scored_many<DH, PAGED, MODE><<<(int)scored_grid(a), 256, 0, s>>>(a);
-  else k_scored_few<DH, PAGED, MODE><<<(int)scored_grid(a), 256, 0, s>>>(a);
+enum class Form { FEW, MANY, ONCE };
+template <Form FORM, int DH, bool PAGED, int MODE> void launch_scored(const ScoredAttn &a, hipStream_t s) {
+  if constexpr (FORM == Form::FEW) k_scored_few<DH, PAGED, MODE><<<(int)scored_grid(a), 256, 0, s>>>(a);
+  else k_scored_many<DH, PAGED, MODE, FORM == Form::ONCE><<<(int)scored_grid(a), 256, 0, s>>>(a);
 }
-template <bool MANY, bool PAGED> void launch_by_shape(const ScoredAttn &a, hipStream_t s) {
+template <Form FORM, bool PAGED> void launch_by_shape(const ScoredAttn &a, hipStream_t s) {
   auto go = [&](auto mode_c) {
     constexpr int MODE = decltype(mode_c)::value;
-    if (a.dh == 64) launch_scored<MANY, 64, PAGED, MODE>(a, s);
-    else launch_scored<MANY, 128, PAGED, MODE>(a, s);
+    if (a.dh == 64) launch_scored<FORM, 64, PAGED, MODE>(a, s);
+    else launch_scored<FORM, 128, PAGED, MODE>(a, s);
   };
   switch (mode_of(a)) {
     case PLAIN: return go(std::integral_constant<int, PLAIN>{});
-    case SHAPED: return go(std::integral_constant<int, SHAPED>{});
-    case DOCS:
-      if constexpr (!PAGED) go(std::integral_constant<int, DOCS>{});
-      return;
+    case CAPPED: return go(std::integral_constant<int, CAPPED>{});
+    case BIASED: return go(std::integral_constant<int, BIASED>{});
+    case CAPPED | BIASED: return go(std::integral_constant<int, CAPPED | BIASED>{});
+  }
+  if constexpr (!PAGED) {
+    if (mode_of(a) == DOCS) go(std::integral_constant<int, DOCS>{});
+    else go(std::integral_constant<int, DOCS_ANY>{});
   }
 }
 

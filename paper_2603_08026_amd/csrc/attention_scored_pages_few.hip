@@ -2,5 +2,5 @@
 #include "attention_scored_kernels.h"
 
 namespace dy {
-void launch_scored_pages_few(const ScoredAttn &a, hipStream_t s) { launch_by_shape<false, true>(a, s); }
+void launch_scored_pages_few(const ScoredAttn &a, hipStream_t s) { launch_by_shape<Form::FEW, true>(a, s); }
 }  // namespace dy

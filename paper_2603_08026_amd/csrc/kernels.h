@@ -245,15 +245,19 @@ struct ScoredAttn {
   int block = 0;
   const int32_t *prefix = nullptr, *doc = nullptr;
   const float *slopes = nullptr;
-  // scratch: partial results of key splits [splits, cap, H, dh] and their (maximum, sum), splits of every row
+  // scratch: partial results of key splits [splits, cap, H, dh] and their (maximum, sum); ARRIVE_WORDS counters, all zero between calls
   float *part_o = nullptr, *part_ml = nullptr;
-  int32_t *n_split = nullptr;
   size_t part_elems = 0;
+  int32_t *arrive = nullptr;
+  int32_t *n_split = nullptr;      // splits of every row, for as many rows as split_rows; nullptr: the splits are not merged by a launch of their own
+  int split_rows = 0;
   int32_t *status = nullptr;
   int bad_page_code = 0;
-  // chosen by scored_plan: rows of a tile, most splits of a sequence, workgroups to split for
+  // chosen by scored_plan: rows of a tile, most splits of a sequence, workgroups to split for, whether the last one merges, copies past the L2
   int bq = 0, splits = 1, target = 0;
+  bool fused = false, once = false;
 };
+constexpr int ARRIVE_WORDS = 4096;
 void scored_plan(DType t, ScoredAttn *a);
 void launch_attention_scored(DType t, const ScoredAttn &a, hipStream_t s);
 // exact rows (a) and the context update of Alg. 4 (b: norm_k) in one launch, where both are bf16 with head_dim 128, one key split

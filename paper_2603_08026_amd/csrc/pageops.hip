@@ -16,18 +16,19 @@ namespace {
 // position lies in.  So the sums are made once a workgroup, in LDS, and rows, taken pages and pages that go back to the list are dealt out
 // by their numbers, each finding its request by a binary search: no workgroup waits for another, long prompts are shared out, and the
 // result does not depend on the order of anything.
-// Bound by the launch and the chain load - scan - search - store.
-constexpr int PLAN_NT = 1024;
+// Bound by the launch and the chain load - scan - search - load - store.
 constexpr int MANY = 1 << 30;  // sums stop here
 __device__ __forceinline__ int sat(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)MANY); }
-__device__ __forceinline__ int sat_scan(int x) {  // inclusive over a wave
-  const int lane = threadIdx.x % WAVE;
-#pragma unroll
-  for (int o = 1; o < WAVE; o *= 2) {
-    const int y = __shfl_up(x, o, WAVE);
-    if (lane >= o) x = sat(x, y);
-  }
-  return x;
+template <int CTRL, int ROWS> __device__ __forceinline__ int sat_step(int x) {
+  return sat(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ int sat_scan(int x) {  // inclusive over a wave, as wave_scan
+  x = sat_step<0x111, 0xf>(x);
+  x = sat_step<0x112, 0xf>(x);
+  x = sat_step<0x114, 0xf>(x);
+  x = sat_step<0x118, 0xf>(x);
+  x = sat_step<0x142, 0xa>(x);
+  return sat_step<0x143, 0xc>(x);
 }
 // first r with v[r] > k, v ascending; n if none
 __device__ __forceinline__ int first_above(const int *v, int n, int k) {
@@ -39,118 +40,127 @@ __device__ __forceinline__ int first_above(const int *v, int n, int k) {
   return lo;
 }
 
-template <int MOST>
-__global__ __launch_bounds__(PLAN_NT) void k_page_plan(Pages pages, PagePlan a) {
-  __shared__ int sums[3 * MOST];  // inclusive sums [R] of rows, gains, losses
-  __shared__ int wave_total[3][PLAN_NT / WAVE], taken_of[PLAN_NT / WAVE];
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, R = a.R;
-  int *rows_to = sums, *gain_to = sums + R, *loss_to = sums + 2 * R;
-  const int shift = pages.shift;
-  const long room = (long)pages.max_pages << shift;  // (below 2^31: checked on the host)
-  struct Req { int len, then, rows, held, need; bool fits; };
-  auto request = [&](int r) {
-    Req q;
-    q.len = (int)min((long)max(a.len[r], 0), room);
+// MOST requests; up to 2048 all that later steps ask of a request lies in LDS, beyond that the sums alone
+template <int NT, int MOST>
+__global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
+  constexpr bool KEPT = MOST <= 2048;
+  constexpr int NW = NT / WAVE;
+  __shared__ int rows_to[MOST], gain_to[MOST], loss_to[MOST];  // inclusive sums
+  __shared__ int kept[KEPT ? 3 * MOST : 1];                    // first position of a row (-1 - that: without room), held, need
+  __shared__ int wave_total[3][NW];
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), R = a.R;
+  const int shift = pages.shift, room = pages.max_pages << shift;  // (at most 2^30: checked on the host)
+  const int free_word = a.n_free[0];
+  struct Req { int start, held, need; bool fits; };  // start: position of its first row
+  struct Full { Req q; int rows, len, then; };
+  auto read = [&](int r) {
+    Full f;
+    f.len = min(max(a.len[r], 0), room);
     const int want = max(a.new_len[r], 0);
-    q.fits = want <= room;
-    q.then = q.fits ? want : q.len;
-    q.rows = min(max(a.new_rows[r], 0), q.then);
-    q.held = (int)(((long)q.len + (1 << shift) - 1) >> shift);
-    q.need = (int)(((long)q.then + (1 << shift) - 1) >> shift);
-    return q;
+    f.q.fits = want <= room;
+    f.then = f.q.fits ? want : f.len;
+    f.rows = min(max(a.new_rows[r], 0), f.then);
+    f.q.start = f.then - f.rows;
+    f.q.held = (f.len + (1 << shift) - 1) >> shift;
+    f.q.need = (f.then + (1 << shift) - 1) >> shift;
+    return f;
+  };
+  auto request = [&](int r) {
+    if constexpr (KEPT) {
+      const int s = kept[r];
+      return Req{s < 0 ? -1 - s : s, kept[MOST + r], kept[2 * MOST + r], s >= 0};
+    } else {
+      return read(r).q;
+    }
   };
   int carry[3] = {0, 0, 0};
   bool unfit = false;
-  for (int r0 = 0; r0 < R; r0 += PLAN_NT) {
+  for (int r0 = 0; r0 < R; r0 += NT) {
     const int r = r0 + tid;
     int x[3] = {0, 0, 0};
     if (r < R) {
-      const Req q = request(r);
-      x[0] = min(q.rows, MANY);
-      x[1] = max(q.need - q.held, 0);
-      x[2] = max(q.held - q.need, 0);
-      unfit = unfit || !q.fits;
+      const Full f = read(r);
+      x[0] = f.rows;
+      x[1] = max(f.q.need - f.q.held, 0);
+      x[2] = max(f.q.held - f.q.need, 0);
+      unfit = unfit || !f.q.fits;
+      if constexpr (KEPT) {
+        kept[r] = f.q.fits ? f.q.start : -1 - f.q.start;
+        kept[MOST + r] = f.q.held;
+        kept[2 * MOST + r] = f.q.need;
+      }
     }
 #pragma unroll
     for (int i = 0; i < 3; ++i) x[i] = sat_scan(x[i]);
-    __syncthreads();
+    if (r0) __syncthreads();
     if (lane == WAVE - 1)
 #pragma unroll
       for (int i = 0; i < 3; ++i) wave_total[i][wave] = x[i];
     __syncthreads();
+    int *to[3] = {rows_to, gain_to, loss_to};
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {  // (the totals of 16 waves, summed up by every wave)
-      const int t = lane < PLAN_NT / WAVE ? wave_total[i][lane] : 0;
-      const int upto = sat_scan(t);
-      const int before = wave ? __builtin_amdgcn_readlane(upto, __builtin_amdgcn_readfirstlane(wave) - 1) : 0;
-      if (r < R) sums[i * R + r] = sat(sat(carry[i], before), x[i]);
-      carry[i] = sat(carry[i], __builtin_amdgcn_readlane(upto, PLAN_NT / WAVE - 1));
+    for (int i = 0; i < 3; ++i) {  // (the totals of the waves, summed up by each of them)
+      const int upto = sat_scan(lane < NW ? wave_total[i][lane] : 0);
+      const int before = wave ? __builtin_amdgcn_readlane(upto, wave - 1) : 0;
+      if (r < R) to[i][r] = sat(sat(carry[i], before), x[i]);
+      carry[i] = sat(carry[i], __builtin_amdgcn_readlane(upto, NW - 1));
     }
   }
   __syncthreads();
-  const int n_rows = carry[0], released = carry[2], n_free = min(max(a.n_free[0], 0), pages.n_pages);
-  const int have = sat(n_free, released);
+  const int released = carry[2], n_free = min(max(free_word, 0), pages.n_pages), have = sat(n_free, released);
   // pages taken: the gains of the served requests, which are a prefix of those that gain
-  int taken = 0;
-  for (int r = tid; r < R; r += PLAN_NT) {
-    const int to = gain_to[r];
-    if (to <= have) taken = max(taken, to);
+  int taken = carry[1];
+  if (taken > have) {
+    const int r = first_above(gain_to, R, have);
+    taken = r ? gain_to[r - 1] : 0;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) taken = max(taken, __shfl_xor(taken, o, WAVE));
-  if (lane == 0) taken_of[wave] = taken;
-  __syncthreads();
-  taken = taken_of[0];
-#pragma unroll
-  for (int w = 1; w < PLAN_NT / WAVE; ++w) taken = max(taken, taken_of[w]);
+  const int n_rows = min(carry[0], a.cap), left = max(released - taken, 0);
+  if (unfit || (tid == 0 && blockIdx.x == 0 && (carry[1] > have || carry[0] > a.cap))) *a.status = a.overflow_code;
 
-  const bool short_of_pages = carry[1] > have, excess = n_rows > a.cap;
-  if ((short_of_pages || excess || unfit) && (blockIdx.x == 0 || unfit)) {
-    if (lane == 0 || unfit) *a.status = a.overflow_code;
-  }
-  const int step = gridDim.x * PLAN_NT, first = blockIdx.x * PLAN_NT + tid;
+  auto before_of = [](const int *v, int r) { return r ? v[r - 1] : 0; };
   auto released_page = [&](int k) {
     const int r = first_above(loss_to, R, k);
-    const Req q = request(r);
-    return pages.table[(size_t)r * pages.max_pages + q.need + (k - (r ? loss_to[r - 1] : 0))];
+    return pages.table[(size_t)r * pages.max_pages + request(r).need + (k - before_of(loss_to, r))];
   };
   auto taken_page = [&](int k) { return k < released ? released_page(k) : a.free_list[n_free - 1 - (k - released)]; };
-  auto served = [&](int r) {
-    const int before = r ? gain_to[r - 1] : 0;
-    return gain_to[r] == before || gain_to[r] <= have;
-  };
-  // rows
-  for (int j = first; j < min(n_rows, a.cap); j += step) {
-    const int r = first_above(rows_to, R, j), before = r ? rows_to[r - 1] : 0;
-    const Req q = request(r);
-    const int p = q.then - q.rows + (j - before), e = p >> shift;
-    a.pos[j] = p;
-    int slot = -1;
-    if (q.fits && served(r)) {
-      const int page = e < q.held ? pages.table[(size_t)r * pages.max_pages + e] : taken_page((r ? gain_to[r - 1] : 0) + (e - q.held));
-      slot = (int)(((uint32_t)page << shift) | (uint32_t)(p & ((1 << shift) - 1)));
+  auto served = [&](int r) { return gain_to[r] <= have || gain_to[r] == before_of(gain_to, r); };
+  // rows, table entries gained, pages that go back, requests: one after the other in number
+  const int total = sat(sat(n_rows, taken), sat(left, R));
+  for (int i = blockIdx.x * NT + tid; i < total; i += gridDim.x * NT) {
+    int k = i;
+    if (k < n_rows) {
+      const int r = first_above(rows_to, R, k);
+      const Req q = request(r);
+      const int p = q.start + (k - before_of(rows_to, r)), e = p >> shift;
+      a.pos[k] = p;
+      int slot = -1;
+      if (q.fits && served(r)) {
+        const int page = e < q.held ? pages.table[(size_t)r * pages.max_pages + e] : taken_page(before_of(gain_to, r) + (e - q.held));
+        slot = (int)(((uint32_t)page << shift) | (uint32_t)(p & ((1 << shift) - 1)));
+      }
+      a.slot[k] = slot;
+      continue;
     }
-    a.slot[j] = slot;
-  }
-  // table entries gained
-  for (int k = first; k < taken; k += step) {
-    const int r = first_above(gain_to, R, k);
-    const Req q = request(r);
-    pages.table[(size_t)r * pages.max_pages + q.held + (k - (r ? gain_to[r - 1] : 0))] = taken_page(k);
-  }
-  // pages that go back
-  for (int k = taken + first; k < released; k += step) {
-    const int to = n_free + (k - taken);
-    if (to < pages.n_pages) a.free_list[to] = released_page(k);
-  }
-  for (int r = first; r < R; r += step) {
-    const Req q = request(r);
-    a.len_out[r] = q.fits && served(r) ? q.then : q.len;
-    a.offsets[r + 1] = min(rows_to[r], a.cap);
-  }
-  if (first == 0) {
-    a.offsets[0] = 0;
-    a.n_free_out[0] = min(have - taken, pages.n_pages);
+    k -= n_rows;
+    if (k < taken) {
+      const int r = first_above(gain_to, R, k);
+      pages.table[(size_t)r * pages.max_pages + request(r).held + (k - before_of(gain_to, r))] = taken_page(k);
+      continue;
+    }
+    k -= taken;
+    if (k < left) {
+      const int at = n_free + k;
+      if (at < pages.n_pages) a.free_list[at] = released_page(taken + k);
+      continue;
+    }
+    k -= left;
+    if (k == 0) {
+      a.offsets[0] = 0;
+      a.n_free_out[0] = min(have - taken, pages.n_pages);
+    }
+    const Full f = read(k);
+    a.len_out[k] = f.q.fits && served(k) ? f.then : f.len;
+    a.offsets[k + 1] = min(rows_to[k], a.cap);
   }
 }
 
@@ -259,12 +269,16 @@ __global__ __launch_bounds__(PH_NT) void k_heads_paged(PagedHeads a, int per, in
 
 }  // namespace
 
+// Rows are shared out over workgroups that each make the sums, so more of them than rows keep busy only add sums.
 void launch_page_plan(const Pages &pages, const PagePlan &a, hipStream_t s) {
   const long work = (long)a.cap + a.R;
-  const long blocks = (work + 2 * PLAN_NT - 1) / (2 * PLAN_NT);
+  const bool small = a.R <= 256;
+  const int nt = small ? 256 : 1024;
+  const long blocks = (work + 2 * nt - 1) / (2 * nt);
   const int grid = (int)(blocks < 1 ? 1 : blocks > 256 ? 256 : blocks);
-  if (a.R <= 1024) k_page_plan<1024><<<grid, PLAN_NT, 0, s>>>(pages, a);
-  else k_page_plan<MAX_REQUESTS><<<grid, PLAN_NT, 0, s>>>(pages, a);
+  if (small) k_page_plan<256, 256><<<grid, 256, 0, s>>>(pages, a);
+  else if (a.R <= 2048) k_page_plan<1024, 2048><<<grid, 1024, 0, s>>>(pages, a);
+  else k_page_plan<1024, MAX_REQUESTS><<<grid, 1024, 0, s>>>(pages, a);
 }
 
 void launch_heads_paged(DType t, const PagedHeads &a, int dh, hipStream_t s) {

@@ -88,7 +88,7 @@ int main(int argc, char **argv) {
   say("negative capacity -1", heads(good, row([&](auto &r) { r.cap = -1; }), 512));
   say("nothing 0", heads(good, dyllm_page_rows{rows.offsets, nullptr, nullptr, 0}, 512));
   say("nothing 0", attend(good, dyllm_page_rows{rows.offsets, nullptr, nullptr, 0}, 2));
-  say("capacity -6", attend(good, row([&](auto &r) { r.cap = 9; }), 2));
+  say("capacity of attention 0", attend(good, row([&](auto &r) { r.cap = 9; }), 2));
   say("capacity of heads 0", heads(good, row([&](auto &r) { r.cap = 9; }), 512));
   // heads
   say("short rows -2", heads(good, rows, 504));
@@ -117,7 +117,7 @@ int main(int argc, char **argv) {
   say("no list -1", dyllm_page_plan(ctx, &good, 2, len, now, num, nullptr, n_free, &mine, len_out, n_out, nullptr));
   say("odd list -1", dyllm_page_plan(ctx, &good, 2, odd(len), now, num, free_list, n_free, &mine, len_out, n_out, nullptr));
   say("no context -1", dyllm_page_plan(nullptr, &good, 2, len, now, num, free_list, n_free, &mine, len_out, n_out, nullptr));
-  say("all tokens -6", dyllm_partial_attention_masked(ctx, q, x, x, nullptr, nullptr, 2, 32, nullptr, out, nullptr));
+  say("all tokens 0", dyllm_partial_attention_masked(ctx, q, x, x, nullptr, nullptr, 2, 32, nullptr, out, nullptr));
   say("sequences -2", dyllm_partial_attention_masked(ctx, q, x, x, nullptr, nullptr, 3, 2, nullptr, out, nullptr));
   say("odd keys -1", dyllm_partial_attention_masked(ctx, q, off(x), x, nullptr, nullptr, 1, 8, nullptr, out, nullptr));
   say("odd lengths -1", dyllm_partial_attention_masked(ctx, q, x, x, odd(kv), nullptr, 1, 8, nullptr, out, nullptr));

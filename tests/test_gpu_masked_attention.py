@@ -301,7 +301,8 @@ def test_what_is_refused():
         with pytest.raises(Bd.DyllmError) as e:
             call()
         assert e.value.code == code
-    refused(-6, lambda: ctx.partial_attention_masked(bf(32, 4, 64), k, k, None, B, L, bf(32, 256)))  # rows None: max_rows has to cover B*L
+    refused(-6, lambda: ctx.partial_attention_masked(bf(9, 4, 64), k, k, Bd.IndexList(ints([0] * 9), rows.offsets), B, L, bf(9, 256)))
+    ctx.partial_attention_masked(bf(32, 4, 64), k, k, None, B, L, bf(32, 256))  # (all tokens need no room in the context)
     refused(-2, lambda: ctx.partial_attention_masked(q, bf(3, L, 2, 64), bf(3, L, 2, 64), Bd.IndexList(rows.idx, ints([0, 1, 2, 2])), 3, L, out))
     refused(-1, lambda: ctx.partial_attention_masked(q, k, k, rows, B, L, out, Bd.Scores(cap=INF)))
     refused(-1, lambda: ctx.partial_attention_masked(bf(2 * 256 + 1)[1:], k, k, rows, B, L, out))

@@ -551,8 +551,6 @@ def test_what_the_binding_refuses():
     refused(-1, lambda: ctx.head_norm_rope_paged(qkv, None, None, rows, p, q, ints(np.zeros((2, 4))), bytes([2] * 32)))
     refused(-1, lambda: ctx.head_norm_rope_paged(qkv, None, None, rows, p, q, ints(np.zeros((9, 4))), sixteen))
     refused(-2, lambda: ctx.head_norm_rope_paged(bf(4, 516)[:, :512], None, None, rows, p, q))
-    many = Bd.PageRows.empty(17, 2)
-    refused(-6, lambda: ctx.paged_attention(bf(17, 4, 64), p, many, z, bf(17, 256)))
     refused(-3, lambda: ctx.paged_attention(q, p, rows, z, out, Bd.Scores(doc=ints([0] * 8))))
     assert ctx.poll_status() == 0
     ctx._dev = 1
