@@ -616,12 +616,15 @@ class Context:
         Of pages the table and the sizes are used."""
         dev, i32 = self._here(), torch.int32
         R = self._requests(length.numel(), rows, pages)
-        p, r = self._pages(pages, dev, False), self._page_rows(rows, dev)
-        self._check(self.lib.dyllm_page_plan(
-            self.h, p, R, self._arg(length, R, "length", dev, i32), self._arg(new_length, R, "new_length", dev, i32),
-            self._arg(new_rows, R, "new_rows", dev, i32), self._arg(free_list, pages.shape[0], "free_list", dev, i32),
-            self._arg(n_free, 1, "n_free", dev, i32), r, self._arg(length_out, R, "length_out", dev, i32),
-            self._arg(n_free_out, 1, "n_free_out", dev, i32), _raw_stream(dev)))
+        lists = (length, new_length, new_rows, length_out, free_list, n_free, n_free_out)
+        for t in lists:  # (in one go: these checks are a third of the call)
+            if t.dtype is not i32 or not t.is_contiguous() or t.get_device() != dev:
+                raise ValueError("page_plan: contiguous int32 tensors on the current device are wanted")
+        if new_length.numel() < R or new_rows.numel() < R or length_out.numel() < R or free_list.numel() < pages.shape[0] or not (n_free.numel() and n_free_out.numel()):
+            raise ValueError("page_plan: %d lengths, rows and lengths out, %d free pages and two counts are wanted" % (R, pages.shape[0]))
+        at = [t.data_ptr() for t in lists]
+        self._check(self.lib.dyllm_page_plan(self.h, self._pages(pages, dev, False), R, at[0], at[1], at[2], at[4], at[5], self._page_rows(rows, dev),
+                                             at[3], at[6], _raw_stream(dev)))
 
     def head_norm_rope_paged(self, qkv, g_q, g_k, rows: PageRows, pages: Pages, q_out, axis_pos=None, axis=None):
         """qkv: [cap, (H + 2 Hkv) dh], rows may be strided; g_q, g_k: [dh] or None.  axis_pos: int32 [n_axes, cap] positions with axis, the axis of
@@ -631,10 +634,11 @@ class Context:
         p, ld = self._qkv(qkv, n, dev)
         q = self._arg(q_out, n * self._dq, "q_out", dev)
         if axis_pos is not None:
-            n_axes = axis_pos.shape[0]
-            if axis_pos.dim() != 2 or axis_pos.shape[1] != n or axis is None or len(axis) != self._dh // 2:
+            shape = axis_pos.shape
+            if len(shape) != 2 or shape[1] != n or axis is None or len(axis) != self._dh // 2:
                 raise ValueError("axis_pos: [n_axes, %d] and an axis for each of %d pairs are wanted" % (n, self._dh // 2))
-            axis_pos, axis = self._arg(axis_pos, n_axes * n, "axis_pos", dev, torch.int32), bytes(axis)
+            n_axes, axis = shape[0], bytes(axis)
+            axis_pos = self._arg(axis_pos, n_axes * n, "axis_pos", dev, torch.int32)
         else:
             axis = None
         self._check(self.lib.dyllm_head_norm_rope_paged(

@@ -42,6 +42,29 @@ __device__ __forceinline__ int position_of(const ScoredAttn &a, bool pages, int 
   return pages ? a.at[j] : (a.at ? a.at[j] : j) - b * a.L;
 }
 
+// Over a wave, with moves between vector registers alone, as wave_scan (a workgroup makes some ten of these before its first copy; through LDS each took 0.3 us).
+template <typename T, typename Op> __device__ __forceinline__ T wave_fold(T x, Op op) {
+  auto step = [&](auto ctrl_c, auto rows_c) {
+    // (a lane that nothing moves to keeps its own: for minima and maxima; sums take the zero)
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const uint32_t old = Op::idempotent ? u : 0u;
+    x = op(x, __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)u, decltype(ctrl_c)::value, decltype(rows_c)::value, 0xf, false)));
+  };
+  using every = std::integral_constant<int, 0xf>;
+  step(std::integral_constant<int, 0x111>{}, every{});
+  step(std::integral_constant<int, 0x112>{}, every{});
+  step(std::integral_constant<int, 0x114>{}, every{});
+  step(std::integral_constant<int, 0x118>{}, every{});
+  step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+  step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_readlane((int)__builtin_bit_cast(uint32_t, x), WAVE - 1));
+}
+struct Least { static constexpr bool idempotent = true; __device__ int operator()(int a, int b) const { return min(a, b); } };
+struct Most { static constexpr bool idempotent = true; __device__ int operator()(int a, int b) const { return max(a, b); } };
+struct Sum { static constexpr bool idempotent = false; __device__ float operator()(float a, float b) const { return a + b; } };
+__device__ __forceinline__ int wave_min_i(int v) { return wave_fold(v, Least{}); }
+__device__ __forceinline__ int wave_max_i(int v) { return wave_fold(v, Most{}); }
+
 // ---- work items: (key-value head, sequence, key split, tile of packed rows) ---------------------------------------
 // The rows of a sequence and the g heads of a group are packed as in the grouped form above.  Where rows are few the keys of a sequence are split, in
 // pieces of one size for all sequences, the smallest with which no more than a.target items are made: workgroups of ragged requests then
@@ -94,7 +117,7 @@ __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
       w += (float)tiles * (float)keys;
     }
     // (a first size from the sum, then what it makes of the sequences' ends; sums of whole numbers, and every workgroup finds the same)
-    float pieces = wave_sum(w) * (float)a.Hkv / (float)a.target;
+    float pieces = wave_fold(w, Sum{}) * (float)a.Hkv / (float)a.target;
 #pragma unroll 1
     for (int round = 0; round < 4; ++round) {
       chunk = max((int)ceilf(fminf(pieces, 1e9f) / SPLIT_KEYS), 1) * SPLIT_KEYS;
@@ -104,7 +127,7 @@ __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
         int size;
         items += (float)(tiles * splits_of(&size));
       }
-      items = wave_sum(items) * (float)a.Hkv;
+      items = wave_fold(items, Sum{}) * (float)a.Hkv;
       if (items <= (float)a.target) break;  // uniform
       pieces = (float)chunk * fmaxf(items / (float)a.target, 1.02f);
     }
@@ -278,17 +301,6 @@ __device__ __forceinline__ const unsigned char *uniform_bytes(const void *p) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
   return (const unsigned char *)(((uint64_t)hi << 32) | lo);
 }
-__device__ __forceinline__ int wave_min_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, WAVE));
-  return __builtin_amdgcn_readfirstlane(v);
-}
-__device__ __forceinline__ int wave_max_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, WAVE));
-  return __builtin_amdgcn_readfirstlane(v);
-}
-
 // Where the keys and values of a sequence and head lie.  A tile of 32 keys starts at a multiple of 32, pages hold a multiple of 16: its two halves
 // lie each in one piece.  PAGED: their pages are asked for through the scalar cache, a tile ahead.
 template <bool PAGED, int DH> struct KeyPlaces {

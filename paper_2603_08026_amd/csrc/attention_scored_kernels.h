@@ -13,7 +13,7 @@ namespace {
 // its own ring in LDS, with no barrier in the loop; their results are merged once at the end.
 template <int DH, int MODE> struct FewTile : KeyTile<DH> {
   using K = KeyTile<DH>;
-  static constexpr int NW = 4, NS = 2, BQ = 32;
+  static constexpr int NW = 4, NS = DH == 128 ? 2 : 4, BQ = 32;
   static constexpr int STAGE = 2 * K::REGION + (MODE & DOCS ? 256 : 0), PER_TILE = 2 * K::COPIES + (MODE & DOCS ? 1 : 0);
   static constexpr int PER_WAVE = (K::DB * 16 + 2) * 64;  // floats of a wave's result
   static constexpr int RING = NS * STAGE, LDS = NW * RING;
@@ -115,7 +115,10 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
   const int vrow = 4 * lhi + (lane % 16) / 4, hb = (lane / 16) & 1;
 
   for (int n = 0; n < n_tiles; ++n) {
-    if (n + 1 < n_tiles) wait_vmcnt<(NS - 1) * T::PER_TILE>();  // tile n has landed
+    // tile n has landed, of those up to n + NS - 1 that exist
+    if (n + NS - 1 < n_tiles) wait_vmcnt<(NS - 1) * T::PER_TILE>();
+    else if (NS > 3 && n + 2 < n_tiles) wait_vmcnt<2 * T::PER_TILE>();
+    else if (NS > 2 && n + 1 < n_tiles) wait_vmcnt<T::PER_TILE>();
     else wait_vmcnt<0>();
     const unsigned char *st = own + (n % NS) * T::STAGE;
     floatx16 s;
@@ -312,6 +315,9 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   float m_run = -INFINITY, l_run = 0.f;
   const float sc = sh.sc;
 
+  // Stage of a tile.  (Where the first tile has keys of another document the second starts the unrolled loop, and has stage 0.)
+  const int turn = (MODE == DOCS) && tests.first > k_lo ? NS - 1 : 0;
+  auto stage = [&](int t) { return (uint32_t)(t + turn) % NS; };
   // Copies: copy c of a wave fills rows (c * NW + wave) * RPC and on.
   const uint32_t lds0 = lds_offset_of(smem);
   KeyPlaces<PAGED, DH> places(a, b, kvh);
@@ -321,7 +327,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   static_assert(CPW == 1 || NW * RPC == 16, "");
   size_t off[2];
   auto one_copy = [&](int t, int c) {  // of a tile all of whose keys exist
-    const uint32_t base = lds0 + (uint32_t)(t % NS) * T::STAGE;
+    const uint32_t base = lds0 + stage(t) * T::STAGE;
     if ((MODE & DOCS) && c == 2 * CPW) {
       dma4(a.doc + (size_t)b * a.L + k_lo + t * TK + l32, base + 2 * T::REGION + wave * 256u);
       return;
@@ -333,7 +339,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
     else dma16_s((c & 1 ? places.v : places.k) + o, c & 1 ? off_v : off_k, to);
   };
   auto last_copies = [&](int t) {  // keys past the end are the last one again, masked later
-    const uint32_t base = lds0 + (uint32_t)(t % NS) * T::STAGE;
+    const uint32_t base = lds0 + stage(t) * T::STAGE;
     const int last = k_hi - 1 - (k_lo + t * TK);
 #pragma unroll
     for (int i = 0; i < CPW; ++i) {
@@ -379,7 +385,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
     for (int e = 0; e < 16; ++e) s_cur[e] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(smem + l32 * ROWB + T::k_chunk(l32, 2 * kk + lhi) * 16);
+      const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(smem + stage(0) * T::STAGE + l32 * ROWB + T::k_chunk(l32, 2 * kk + lhi) * 16);
       s_cur = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], s_cur, 0, 0, 0);
     }
     // V^T and the rounded probabilities of the tile whose product is still to be issued (zero before the first)
@@ -400,7 +406,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       constexpr int TEST = decltype(test_c)::value;
       constexpr bool CLEAN = TEST == NOTHING;
       constexpr int STAGE = decltype(stage_c)::value;
-      const int sidx = STAGE >= 0 ? STAGE : t % NS;
+      const int sidx = STAGE >= 0 ? STAGE : (int)stage(t);
       const bool more = CLEAN || t + NS - 1 < n_tiles, spread = CLEAN || (more && full(t + NS - 1));
       if (CLEAN) wait_vmcnt<(NS - 3) * LPW>();
       else landed_next(t);
@@ -517,10 +523,10 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       for (; t < n_mine; ++t) one(t, all{});
     } else {
       if constexpr (MODE == DOCS) {
-        const int n_all = tests.solid ? (tests.first > k_lo ? min(NS, n_mine) : 0) : n_mine;  // (solid: the first tile may have keys of another document)
+        const int n_all = tests.solid ? (tests.first > k_lo ? 1 : 0) : n_mine;  // (solid: the first tile may have keys of another document)
         for (; t < n_all; ++t) one(t, all{});
       }
-      for (; t + NS <= n_fast; t += NS) {  // t % NS == 0 here
+      for (; t + NS <= n_fast; t += NS) {  // stage(t) == 0 here
         body(t, nothing{}, std::integral_constant<int, 0>{});
         body(t + 1, nothing{}, std::integral_constant<int, 1>{});
         body(t + 2, nothing{}, std::integral_constant<int, 2>{});
