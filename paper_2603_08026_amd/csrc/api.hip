@@ -46,6 +46,7 @@ struct dyllm_ctx {
   int32_t *plan, *plan_up, *plan_down, *plan_kv;
   int32_t *scan;   // words of the chained compaction kernel; all zero between calls
   int32_t *arrive; // counters of attention's key splits (ARRIVE_WORDS); all zero between calls
+  int32_t *list;   // work of attention over many sequences
   float *rope;     // [max_seq, dh/2, 2]
   uint64_t turns[64];  // what a pair of columns is turned by a position, in 2^-64 turns
   // optional per-stage timing (dyllm_profile_begin / _end)
@@ -58,7 +59,7 @@ struct dyllm_ctx {
 namespace {
 
 struct Layout {
-  size_t ns, qs, part_o, part_ml, cosb, flag, hs, fs, act, status, rope, dv_full, dc, csal, pos, win_idx, win_off, ksal, scan, arrive, total;
+  size_t ns, qs, part_o, part_ml, cosb, flag, hs, fs, act, status, rope, dv_full, dc, csal, pos, win_idx, win_off, ksal, scan, arrive, list, total;
   size_t part_elems, quant_part_elems;
 };
 
@@ -104,6 +105,7 @@ Layout make_layout(const dyllm_layer_cfg &c) {
   l.ksal = take(R * dkv * e);
   l.scan = take((size_t)compact_scan_words() * 4);
   l.arrive = take((size_t)ARRIVE_WORDS * 4);
+  l.list = take((1 + 2 * (size_t)std::max(c.max_batch, MAX_REQUESTS)) * 4);
   l.total = off;
   return l;
 }
@@ -692,7 +694,7 @@ ScoredAttn scored_args(const dyllm_ctx *ctx, const void *q, const dyllm_scores *
   a.H = c.n_heads; a.Hkv = c.n_kv_heads; a.dh = c.head_dim;
   if (sc) { a.soft_cap = sc->cap; a.block = sc->block; a.prefix = sc->prefix; a.slopes = sc->slopes; a.doc = sc->doc; }
   a.part_o = ctx->part_o; a.part_ml = ctx->part_ml; a.part_elems = ctx->quant_part_elems;
-  a.arrive = ctx->arrive;
+  a.arrive = ctx->arrive; a.list = ctx->list;
   a.n_split = (int32_t *)ctx->cosb; a.split_rows = ctx->rows_cap;
   a.status = ctx->status; a.bad_page_code = DYLLM_ERR_INVALID_ARG;
   return a;
@@ -759,6 +761,7 @@ int dyllm_create(const dyllm_layer_cfg *cfg, dyllm_ctx **out) {
   ctx->win_idx = (int32_t *)(b + l.win_idx); ctx->win_off = (int32_t *)(b + l.win_off);
   ctx->ksal = b + l.ksal; ctx->scan = (int32_t *)(b + l.scan);
   ctx->arrive = (int32_t *)(b + l.arrive);
+  ctx->list = (int32_t *)(b + l.list);
 
   // rotary table in double precision on the host, cleared status word
   const int half = cfg->head_dim / 2;

@@ -89,103 +89,102 @@ struct ScoredItem {
   int kv_head = 0, keys = 0, split = 0, splits = 1, chunk = 0;
   int counter = 0;  // number of the (tile, key-value head)
 };
-__device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
-  const int g = a.H / a.Hkv, lane = threadIdx.x % WAVE, BQ = a.bq;
-  ScoredItem it;
-  const int total = a.offsets ? min(a.offsets[a.B], a.cap) : a.B * a.L;
-  int lo = 0, hi = 0, tiles = 0, keys = 0;
-  auto look = [&](int b0) {  // this lane's sequence
-    const int b = b0 + lane;
-    lo = hi = tiles = keys = 0;
-    if (b < a.B) {
-      lo = a.offsets ? min(max(a.offsets[b], 0), total) : b * a.L;
-      hi = a.offsets ? max(min(a.offsets[b + 1], total), lo) : lo + a.L;
-      tiles = ((hi - lo) * g + BQ - 1) / BQ;
-      keys = keys_of(a, b);
-    }
-  };
-  int chunk = 0x7fffff80;
-  auto splits_of = [&](int *size) {
-    const int least = ((keys + a.splits - 1) / a.splits + SPLIT_KEYS - 1) / SPLIT_KEYS * SPLIT_KEYS;
-    *size = max(chunk, least);
-    return max(1, (int)(((long)keys + *size - 1) / *size));
-  };
-  if (a.splits > 1) {
-    float w = 0.f;
-    for (int b0 = 0; b0 < a.B; b0 += WAVE) {
-      look(b0);
-      w += (float)tiles * (float)keys;
-    }
-    // (a first size from the sum, then what it makes of the sequences' ends; sums of whole numbers, and every workgroup finds the same)
-    float pieces = wave_fold(w, Sum{}) * (float)a.Hkv / (float)a.target;
+struct ScoredSeq { int lo = 0, rows = 0, tiles = 0, keys = 0; };
+__device__ __forceinline__ int scored_rows(const ScoredAttn &a) { return a.offsets ? min(a.offsets[a.B], a.cap) : a.B * a.L; }
+__device__ __forceinline__ ScoredSeq scored_seq(const ScoredAttn &a, int b, int total) {
+  ScoredSeq q;
+  if (b >= a.B) return q;
+  q.lo = a.offsets ? min(max(a.offsets[b], 0), total) : b * a.L;
+  q.rows = a.offsets ? max(min(a.offsets[b + 1], total), q.lo) - q.lo : a.L;
+  q.tiles = (q.rows * (a.H / a.Hkv) + a.bq - 1) / a.bq;
+  q.keys = keys_of(a, b);
+  return q;
+}
+// keys of a split of a sequence (no more than a.splits of them), and how many splits that makes
+__device__ __forceinline__ int split_size(const ScoredAttn &a, int keys, int chunk) {
+  return max(chunk, ((keys + a.splits - 1) / a.splits + SPLIT_KEYS - 1) / SPLIT_KEYS * SPLIT_KEYS);
+}
+__device__ __forceinline__ int split_count(int keys, int size) { return max(1, (int)(((long)keys + size - 1) / size)); }
+constexpr int WHOLE = 0x7fffff80;  // a piece that holds any sequence
+// A first size from the sum of tiles * keys, then what it makes of the sequences' ends.  sum: (function of a sequence -> number) -> its sum over all of
+// them; sums of whole numbers in a fixed order, every workgroup finds the same.
+template <typename SUM> __device__ __forceinline__ int scored_chunk(const ScoredAttn &a, SUM &&sum) {
+  if (a.splits <= 1) return WHOLE;
+  int chunk = WHOLE;
+  float pieces = sum([&](const ScoredSeq &q) { return (float)q.tiles * (float)q.keys; }) * (float)a.Hkv / (float)a.target;
 #pragma unroll 1
-    for (int round = 0; round < 4; ++round) {
-      chunk = max((int)ceilf(fminf(pieces, 1e9f) / SPLIT_KEYS), 1) * SPLIT_KEYS;
-      float items = 0.f;
-      for (int b0 = 0; b0 < a.B; b0 += WAVE) {
-        if (a.B > WAVE) look(b0);
-        int size;
-        items += (float)(tiles * splits_of(&size));
-      }
-      items = wave_fold(items, Sum{}) * (float)a.Hkv;
-      if (items <= (float)a.target) break;  // uniform
-      pieces = (float)chunk * fmaxf(items / (float)a.target, 1.02f);
-    }
+  for (int round = 0; round < 4; ++round) {
+    chunk = max((int)ceilf(fminf(pieces, 1e9f) / SPLIT_KEYS), 1) * SPLIT_KEYS;
+    const float items = sum([&](const ScoredSeq &q) { return (float)(q.tiles * split_count(q.keys, split_size(a, q.keys, chunk))); }) * (float)a.Hkv;
+    if (items <= (float)a.target) break;  // uniform
+    pieces = (float)chunk * fmaxf(items / (float)a.target, 1.02f);
   }
-  int size = 0, upto = 0, tiles_to = 0, n_items = 0, n_tiles = 0;
-  for (int b0 = 0; b0 < a.B; b0 += WAVE) {
-    if (a.B > WAVE || a.splits == 1) look(b0);
-    upto = wave_scan(tiles * splits_of(&size));
-    tiles_to = wave_scan(tiles);
-    n_items += __builtin_amdgcn_readlane(upto, WAVE - 1);
-    n_tiles += __builtin_amdgcn_readlane(tiles_to, WAVE - 1);
-  }
+  return chunk;
+}
+// item p of the grid -> key-value head and item of that head, of n_items
+__device__ __forceinline__ bool scored_place(const ScoredAttn &a, int p, int n_items, int *kv_head, int *w) {
+  if (n_items == 0) return false;
   const int x = p % ATTN_XCD, s = p / ATTN_XCD;
-  int w;
-  if (n_items == 0) return it;
   if (a.Hkv % ATTN_XCD == 0) {
     const int per = a.Hkv / ATTN_XCD;
-    if (s / n_items >= per) return it;
-    it.kv_head = x * per + s / n_items;
-    w = s % n_items;
-  } else if (ATTN_XCD % a.Hkv == 0) {
+    *kv_head = x * per + s / n_items;
+    *w = s % n_items;
+    return s / n_items < per;
+  }
+  if (ATTN_XCD % a.Hkv == 0) {
     const int per = ATTN_XCD / a.Hkv;
-    it.kv_head = x / per;
-    w = s * per + x % per;
-    if (w >= n_items) return it;
-  } else {
-    const long items = (long)n_items * a.Hkv, per_xcd = (items + ATTN_XCD - 1) / ATTN_XCD, at = x * per_xcd + s;
-    if (s >= per_xcd || at >= items) return it;
-    it.kv_head = (int)(at / n_items);
-    w = (int)(at % n_items);
+    *kv_head = x / per;
+    *w = s * per + x % per;
+    return *w < n_items;
   }
-  it.counter = it.kv_head * n_tiles;
-  for (int b0 = 0; b0 < a.B; b0 += WAVE) {
-    if (a.B > WAVE) {
-      look(b0);
-      upto = wave_scan(tiles * splits_of(&size));
-      tiles_to = wave_scan(tiles);
-    }
-    const uint64_t past = __ballot(upto > w);
-    if (past) {
-      const int f = __ffsll((unsigned long long)past) - 1;
-      const int nt = __builtin_amdgcn_readlane(tiles, f), rows = __builtin_amdgcn_readlane(hi - lo, f);
-      it.seq = b0 + f;
-      it.row = __builtin_amdgcn_readlane(lo, f);
-      it.keys = __builtin_amdgcn_readlane(keys, f);
-      it.chunk = __builtin_amdgcn_readlane(size, f);
-      it.splits = max(1, (int)(((long)it.keys + it.chunk - 1) / it.chunk));
-      const int mine = w - (__builtin_amdgcn_readlane(upto, f) - nt * it.splits);
-      it.split = mine / nt;
-      const int tile = nt - 1 - mine % nt;  // the last rows of a causal sequence have the most keys: they come first
-      it.counter += __builtin_amdgcn_readlane(tiles_to, f) - nt + tile;
-      it.packed = tile * BQ;
-      it.n = min(BQ, rows * g - it.packed);
-      return it;
-    }
-    w -= __builtin_amdgcn_readlane(upto, WAVE - 1);
-    it.counter += __builtin_amdgcn_readlane(tiles_to, WAVE - 1);
+  const long items = (long)n_items * a.Hkv, per_xcd = (items + ATTN_XCD - 1) / ATTN_XCD, at = x * per_xcd + s;
+  *kv_head = (int)(at / n_items);
+  *w = (int)(at % n_items);
+  return s < per_xcd && at < items;
+}
+// mine: item of the sequence; tiles_before: tiles of the sequences before it
+__device__ __forceinline__ void scored_fill(const ScoredAttn &a, ScoredItem &it, const ScoredSeq &q, int chunk, int mine, int tiles_before, int n_tiles) {
+  it.row = q.lo;
+  it.keys = q.keys;
+  it.chunk = split_size(a, q.keys, chunk);
+  it.splits = split_count(q.keys, it.chunk);
+  it.split = mine / q.tiles;
+  const int tile = q.tiles - 1 - mine % q.tiles;  // the last rows of a causal sequence have the most keys: they come first
+  it.counter = min(it.kv_head * n_tiles + tiles_before + tile, ARRIVE_WORDS - 1);  // (more tiles than the host counted: offsets that do not ascend)
+  it.packed = tile * a.bq;
+  it.n = min(a.bq, q.rows * (a.H / a.Hkv) - it.packed);
+}
+// Up to 64 sequences: every workgroup looks at all of them, a lane at one.  More: k_scored_list has left, for every sequence, the items and tiles of it and
+// those before it, and the size of the pieces; a search over 64 equal parts, then inside one.
+constexpr int LIST_HEAD = 1;  // words before the two lists: the size of the pieces
+__device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
+  const int lane = threadIdx.x % WAVE, total = scored_rows(a);
+  ScoredItem it;
+  int w;
+  if (a.B <= WAVE) {
+    const ScoredSeq q = scored_seq(a, lane, total);
+    const int chunk = scored_chunk(a, [&](auto f) { return wave_fold(f(q), Sum{}); });
+    const int upto = wave_scan(q.tiles * split_count(q.keys, split_size(a, q.keys, chunk))), tiles_to = wave_scan(q.tiles);
+    if (!scored_place(a, p, __builtin_amdgcn_readlane(upto, WAVE - 1), &it.kv_head, &w)) return it;
+    const int f = __ffsll((unsigned long long)__ballot(upto > w)) - 1;
+    const int before = f ? __builtin_amdgcn_readlane(upto, f - 1) : 0, tiles_before = f ? __builtin_amdgcn_readlane(tiles_to, f - 1) : 0;
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, f); };
+    it.seq = f;
+    scored_fill(a, it, ScoredSeq{of(q.lo), of(q.rows), of(q.tiles), of(q.keys)}, chunk, w - before, tiles_before, __builtin_amdgcn_readlane(tiles_to, WAVE - 1));
+    return it;
   }
+  const int32_t *items_to = a.list + LIST_HEAD, *tiles_to = items_to + a.B;
+  const int step = (a.B + WAVE - 1) / WAVE, chunk = a.list[0], n_tiles = tiles_to[a.B - 1];
+  const int part_end = items_to[min((lane + 1) * step, a.B) - 1];
+  if (!scored_place(a, p, __builtin_amdgcn_readlane(part_end, WAVE - 1), &it.kv_head, &w)) return it;
+  const int part = __ffsll((unsigned long long)__ballot(part_end > w)) - 1;
+  for (int r0 = part * step; it.seq < 0; r0 += WAVE) {  // (the part's end is past w, so one is found)
+    if (r0 >= a.B) return it;
+    const uint64_t past = __ballot(items_to[min(r0 + lane, a.B - 1)] > w);
+    if (past) it.seq = __builtin_amdgcn_readfirstlane(r0 + __ffsll((unsigned long long)past) - 1);
+  }
+  const ScoredSeq q = scored_seq(a, it.seq, total);
+  scored_fill(a, it, q, chunk, w - (it.seq ? items_to[it.seq - 1] : 0), it.seq ? tiles_to[it.seq - 1] : 0, n_tiles);
   return it;
 }
 
@@ -205,8 +204,9 @@ __device__ __forceinline__ float2 load_through(const float *p) {
 // what a row's keys sum up to -> what its values are multiplied by (a row without keys: zero)
 __device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.0f / l; }
 
-// Called by all 256 threads, whose partial results are stored (not waited for); at most 8 rows.  flag: a word of LDS; buf: 4 * DH floats of it.
-// A row is taken by four waves, by two or by one, a wave takes up to two rows at a time: 16 splits of each are in flight.
+// Called by all 256 threads, whose partial results are stored (not waited for).  flag: a word of LDS; buf: 4 * DH floats of it.
+// Eight rows at a time (a tile has more where one sequence has most of the rows); a row is taken by four waves, by two or by one, a wave takes up to
+// two of the eight: 16 splits of each are in flight.
 constexpr int FUSED_ROWS = 8;
 template <typename T, int DH> __device__ __forceinline__ void merge_splits_last(const ScoredAttn &a, const ScoredItem &item, int *flag, float *buf) {
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), grp = a.H / a.Hkv, splits = item.splits;
@@ -228,70 +228,71 @@ template <typename T, int DH> __device__ __forceinline__ void merge_splits_last(
       x[0] = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   };
-  const int parts = item.n == 1 ? 4 : item.n == 2 ? 2 : 1, first = wave / parts, part = wave % parts;  // waves of a row
-  if (first >= item.n) return;  // (only where a wave takes rows alone)
+  const int parts = item.n == 1 ? 4 : item.n == 2 ? 2 : 1, part = wave % parts;  // waves of a row
   const size_t step = (size_t)a.cap * a.H;
-  const bool second = first + 4 < item.n;
-  size_t at[2];
-  float m[2][2], l[2][2], o[2][V], total[2];
+  for (int first = wave / parts; first < item.n; first += FUSED_ROWS) {  // (once where waves share rows)
+    const bool second = first + 4 < item.n;
+    size_t at[2];
+    float m[2][2], l[2][2], o[2][V], total[2];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int p = item.packed + (u && second ? first + 4 : first);
-    at[u] = (size_t)(item.row + p / grp) * a.H + item.kv_head * grp + p % grp;
+    for (int u = 0; u < 2; ++u) {
+      const int p = item.packed + (u && second ? first + 4 : first);
+      at[u] = (size_t)(item.row + p / grp) * a.H + item.kv_head * grp + p % grp;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int s = lane + h * WAVE;
-      const float2 ml = s < splits ? load_through(a.part_ml + (s * step + at[u]) * 2) : float2{-INFINITY, 0.f};
-      m[u][h] = ml.x; l[u][h] = ml.y;
+      for (int h = 0; h < 2; ++h) {
+        const int s = lane + h * WAVE;
+        const float2 ml = s < splits ? load_through(a.part_ml + (s * step + at[u]) * 2) : float2{-INFINITY, 0.f};
+        m[u][h] = ml.x; l[u][h] = ml.y;
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) o[u][e] = 0.f;
     }
 #pragma unroll
-    for (int e = 0; e < V; ++e) o[u][e] = 0.f;
-  }
+    for (int u = 0; u < 2; ++u) {  // m becomes the weights
+      const float M = wave_max(fmaxf(m[u][0], m[u][1])), ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {  // m becomes the weights
-    const float M = wave_max(fmaxf(m[u][0], m[u][1])), ref = M == -INFINITY ? 0.f : M;
+      for (int h = 0; h < 2; ++h) m[u][h] = __builtin_amdgcn_exp2f(m[u][h] - ref);
+      total[u] = wave_sum(l[u][0] * m[u][0] + l[u][1] * m[u][1]);
+    }
+    auto rows = [&](auto count_c) {
+      constexpr int N = decltype(count_c)::value;
+      for (int s0 = part; s0 < splits; s0 += IN_FLIGHT * parts) {  // (past the end the last split again, with no weight)
+        float x[N][IN_FLIGHT][V];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) m[u][h] = __builtin_amdgcn_exp2f(m[u][h] - ref);
-    total[u] = wave_sum(l[u][0] * m[u][0] + l[u][1] * m[u][1]);
-  }
-  auto rows = [&](auto count_c) {
-    constexpr int N = decltype(count_c)::value;
-    for (int s0 = part; s0 < splits; s0 += IN_FLIGHT * parts) {  // (past the end the last split again, with no weight)
-      float x[N][IN_FLIGHT][V];
+        for (int i = 0; i < IN_FLIGHT; ++i)
 #pragma unroll
-      for (int i = 0; i < IN_FLIGHT; ++i)
+          for (int u = 0; u < N; ++u) load(a.part_o + (min(s0 + i * parts, splits - 1) * step + at[u]) * DH + lane * V, x[u][i]);
 #pragma unroll
-        for (int u = 0; u < N; ++u) load(a.part_o + (min(s0 + i * parts, splits - 1) * step + at[u]) * DH + lane * V, x[u][i]);
+        for (int i = 0; i < IN_FLIGHT; ++i) {
+          const int s = s0 + i * parts;
+          if (s >= splits) break;  // uniform
 #pragma unroll
-      for (int i = 0; i < IN_FLIGHT; ++i) {
-        const int s = s0 + i * parts;
-        if (s >= splits) break;  // uniform
+          for (int u = 0; u < N; ++u) {
+            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s < WAVE ? m[u][0] : m[u][1]), s % WAVE));
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-          const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s < WAVE ? m[u][0] : m[u][1]), s % WAVE));
-#pragma unroll
-          for (int e = 0; e < V; ++e) o[u][e] = fmaf(x[u][i][e], w, o[u][e]);
+            for (int e = 0; e < V; ++e) o[u][e] = fmaf(x[u][i][e], w, o[u][e]);
+          }
         }
       }
+    };
+    if (second) rows(std::integral_constant<int, 2>{});
+    else rows(std::integral_constant<int, 1>{});
+    if (parts > 1) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) buf[(wave * V + e) * WAVE + lane] = o[0][e];
+      __syncthreads();
+      if (part > 0) return;
+      for (int w = 1; w < parts; ++w)
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[0][e] += buf[((wave + w) * V + e) * WAVE + lane];
     }
-  };
-  if (second) rows(std::integral_constant<int, 2>{});
-  else rows(std::integral_constant<int, 1>{});
-  if (parts > 1) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) buf[(wave * V + e) * WAVE + lane] = o[0][e];
-    __syncthreads();
-    if (part > 0) return;
-    for (int w = 1; w < parts; ++w)
+    for (int u = 0; u < 2; ++u) {
+      if (u && !second) break;
+      const float inv = inverse_of(total[u]);
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[0][e] += buf[((wave + w) * V + e) * WAVE + lane];
-  }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    if (u && !second) break;
-    const float inv = inverse_of(total[u]);
-#pragma unroll
-    for (int e = 0; e < V; ++e) ((T *)a.out)[at[u] * DH + lane * V + e] = from_f<T>(o[u][e] * inv);
+      for (int e = 0; e < V; ++e) ((T *)a.out)[at[u] * DH + lane * V + e] = from_f<T>(o[u][e] * inv);
+    }
   }
 }
 

@@ -217,6 +217,54 @@ template <int DH, int R> void launch_f32(const ScoredAttn &a, hipStream_t s) {
   else k_scored_f32<DH, false, R><<<(int)scored_grid(a), 256, 0, s>>>(a);
 }
 
+// ---- work of more than 64 sequences ------------------------------------------------------------------------------
+// One workgroup, a thread to a run of neighbouring sequences: the size of the pieces, then items and tiles up to every sequence by one scan.
+// (With every workgroup of the attention going over all sequences instead: LISTFIGS)
+constexpr int LIST_NT = 1024, LIST_NW = LIST_NT / WAVE;
+__global__ __launch_bounds__(LIST_NT) void k_scored_list(ScoredAttn a) {
+  __shared__ float sums[LIST_NW];
+  __shared__ int ends[2][LIST_NW];
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+  const int total = scored_rows(a), per = (a.B + LIST_NT - 1) / LIST_NT, first = tid * per;
+  const int chunk = scored_chunk(a, [&](auto f) {
+    float x = 0.f;
+    for (int i = 0; i < per; ++i) x += f(scored_seq(a, first + i, total));  // (a sequence that is not there has no tiles)
+    x = wave_fold(x, Sum{});
+    if (lane == 0) sums[wave] = x;
+    __syncthreads();
+    x = wave_fold(lane < LIST_NW ? sums[lane] : 0.f, Sum{});
+    __syncthreads();
+    return x;
+  });
+  int n[2] = {0, 0};
+  for (int i = 0; i < per; ++i) {
+    const ScoredSeq q = scored_seq(a, first + i, total);
+    n[0] += q.tiles * split_count(q.keys, split_size(a, q.keys, chunk));
+    n[1] += q.tiles;
+  }
+  int upto[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    upto[k] = wave_scan(n[k]);
+    if (lane == WAVE - 1) ends[k][wave] = upto[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int waves = wave_scan(lane < LIST_NW ? ends[k][lane] : 0);
+    upto[k] += (wave ? __builtin_amdgcn_readlane(waves, wave - 1) : 0) - n[k];
+  }
+  if (tid == 0) a.list[0] = chunk;
+  int32_t *items_to = a.list + LIST_HEAD, *tiles_to = items_to + a.B;
+  for (int i = 0; i < per && first + i < a.B; ++i) {
+    const ScoredSeq q = scored_seq(a, first + i, total);
+    upto[0] += q.tiles * split_count(q.keys, split_size(a, q.keys, chunk));
+    upto[1] += q.tiles;
+    items_to[first + i] = upto[0];
+    tiles_to[first + i] = upto[1];
+  }
+}
+
 // ---- merge of the splits of many rows: a wave to a (row, head), its lanes the splits' weights, then the columns ------------
 // Bound by the latency of its dependent reads.
 template <int DH>
@@ -323,6 +371,7 @@ void scored_plan(DType t, ScoredAttn *a) {
 
 void launch_attention_scored(DType t, const ScoredAttn &a, hipStream_t s) {
   if (a.cap <= 0) return;
+  if (a.B > WAVE) k_scored_list<<<1, LIST_NT, 0, s>>>(a);
   if (t == F32) {
     if (a.dh == 64) launch_f32<64, 2>(a, s);
     else launch_f32<128, 2>(a, s);

@@ -249,6 +249,7 @@ struct ScoredAttn {
   float *part_o = nullptr, *part_ml = nullptr;
   size_t part_elems = 0;
   int32_t *arrive = nullptr;
+  int32_t *list = nullptr;         // of more than 64 sequences: 1 + 2 B words for the call's work
   int32_t *n_split = nullptr;      // splits of every row, for as many rows as split_rows; nullptr: the splits are not merged by a launch of their own
   int split_rows = 0;
   int32_t *status = nullptr;

@@ -115,6 +115,20 @@ def test_key_splits():
             check(44, t, 4, 2, dh, 2, 3001, (3, 1), kind, docs)
 
 
+@pytest.mark.parametrize("t,dh", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_key_splits_of_one_sequence_with_most_rows(t, dh):
+    say("masked attention, key splits of full tiles", t, dh)
+    check(47, t, 4, 2, dh, 2, 3001, (8, 0), "causal")
+    check(47, t, 2, 2, dh, 3, 2000, (1, 21, 2), "prefix")
+
+
+@pytest.mark.parametrize("t,dh", [("bf16", 64), ("f32", 64)])
+def test_more_sequences_than_lanes(t, dh):
+    say("masked attention, 70 sequences", t, dh)
+    check(48, t, 2, 1, dh, 70, 33, tuple((0, 33, 5, 1)[b % 4] for b in range(70)), "causal")
+    check(48, t, 2, 1, dh, 70, 33, tuple((2, 7, 1)[b % 3] for b in range(70)), "block", "runs")
+
+
 def test_plain_scores_are_those_of_partial_attention():
     """Scores that change nothing: each form within its own tolerance of the other."""
     say("masked attention, nothing masked")

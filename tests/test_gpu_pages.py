@@ -377,6 +377,29 @@ def test_attention_of_many_requests(t, room):
     check_paged(24, t, 4, 2, 64, 16, lengths, [min(n, 1) for n in lengths], "causal", room=max(room, 130))
 
 
+@pytest.mark.parametrize("t,H,Hkv,dh,lengths,counts", [
+    ("bf16", 4, 4, 64, (2500, 700, 900, 3000), (1, 1, 1, 29)), ("bf16", 28, 4, 128, (4000,) + (300,) * 7, (8,) + (0,) * 7), ("bf16", 2, 2, 128, (5000, 9), (16, 0)),
+    ("bf16", 8, 2, 64, (3000, 200, 50), (0, 3, 3)), ("f32", 4, 2, 64, (900, 2500), (19, 1))])
+def test_attention_of_a_chunk_beside_single_tokens(t, H, Hkv, dh, lengths, counts):
+    """Few rows a request as a mean, but one request has most of them: its tiles are full, and their keys split."""
+    say("paged attention, a chunk beside single tokens", t, H, Hkv, dh, counts)
+    check_paged(25, t, H, Hkv, dh, 16, list(lengths), list(counts), "causal")
+
+
+@pytest.mark.parametrize("R", [64, 65, 128, 129, 1100])
+@pytest.mark.parametrize("t,H,Hkv,dh", [("bf16", 4, 1, 64), ("bf16", 2, 2, 128), ("f32", 2, 1, 64)])
+def test_attention_of_more_requests_than_lanes(t, H, Hkv, dh, R):
+    """Requests without rows and without keys among them, runs of such, and a long one that is split."""
+    say("paged attention, requests", t, H, Hkv, dh, R)
+    g = W.philox(26, R)
+    lengths = [int(x) for x in g.integers(0, 40, R)]
+    counts = [min(n, int(c)) for n, c in zip(lengths, g.choice([0, 1, 1, 3], R))]
+    for i in list(range(10, 50)) + list(range(R - 3, R)):
+        counts[i] = 0
+    lengths[5], counts[5], lengths[R - 4], counts[R - 4] = 1500, 2, 1100, 40
+    check_paged(26, t, H, Hkv, dh, 16, lengths, counts, "causal", cap=sum(counts) + 9)
+
+
 @pytest.mark.parametrize("H,Hkv", [(24, 24), (10, 5), (16, 8), (12, 3)])
 def test_attention_with_every_order_of_heads(H, Hkv):
     """Head counts that the eight dies share in each of the ways; a chunk of some tiles, causal."""
