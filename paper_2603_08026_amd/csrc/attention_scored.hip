@@ -219,7 +219,8 @@ template <int DH, int R> void launch_f32(const ScoredAttn &a, hipStream_t s) {
 
 // ---- work of more than 64 sequences ------------------------------------------------------------------------------
 // One workgroup, a thread to a run of neighbouring sequences: the size of the pieces, then items and tiles up to every sequence by one scan.
-// (With every workgroup of the attention going over all sequences instead: LISTFIGS)
+// (With every workgroup of the attention going over all sequences instead, one token of each of 1500 requests of 512 keys, 28 heads over 4: 542 us,
+// 270 with the list; of 8192 of 64 keys 8788 / 547; of 128 of 2048 88 / 88.)
 constexpr int LIST_NT = 1024, LIST_NW = LIST_NT / WAVE;
 __global__ __launch_bounds__(LIST_NT) void k_scored_list(ScoredAttn a) {
   __shared__ float sums[LIST_NW];
@@ -326,7 +327,8 @@ void launch_merge(const ScoredAttn &a, hipStream_t s) {
 // The prices are fits to launches of 1 to 16 sequences of 512 to 8192 keys and 1 to 100 rows (32 heads of 128, 28 over 4, 8 over 2 of 64), ns of a key
 // of a sequence: in a workgroup that has its CU alone, what each adds where there are more than CUs, and the way of all keys from memory.
 // Of nine choices each (both forms, 1 split or about 128, 256, 384 and 512 workgroups) the one taken is 4 % slower than the best in the geometric
-// mean of 108 shapes.  A few, 32 / 128 rows without splits / as chosen, us: one token of one sequence of 8192 keys, 32 heads, 85 / 126 / 31; in each of
+// mean of 108 shapes.  (Beyond two workgroups a CU pieces pay only where without them a few CUs had two: one token of 66 requests of 4096 keys, 4 heads,
+// 150 -> 111 us; of 9 of 8192, 32 heads, 263 -> 199; but of 100 of 2048, 4 heads, 73 -> 88, which the 1.15 keeps whole.)  A few, 32 / 128 rows without splits / as chosen, us: one token of one sequence of 8192 keys, 32 heads, 85 / 126 / 31; in each of
 // 16, 28 heads over 4, 91 / 127 / 51; 100 rows of each of 16 of 2048 159 / 68 / 68; 8 heads over 2 of 64, 100 rows of 2048 keys 19.4 / 33 / 17.
 void scored_plan(DType t, ScoredAttn *a) {
   const long g = a->H / a->Hkv, rows = a->offsets ? ((long)a->cap + a->B - 1) / a->B : a->L, packed = rows * g;
@@ -346,9 +348,9 @@ void scored_plan(DType t, ScoredAttn *a) {
     const bool fused = packed <= FUSED_ROWS || f.bq <= FUSED_ROWS;
     for (int s = 1; s == 1 || s <= most; s += s < 8 ? 1 : s / 4) {
       const double m = n * s;
-      if (s > 1 && (m > 512 || (!fused && a->cap > a->split_rows))) break;
+      if (s > 1 && (m > 1024 || (!fused && a->cap > a->split_rows))) break;
       const double rounds = f.each * (m > 256 ? 256 * ceil(m / 256) : m);  // (a CU with two workgroups where others have one ends last)
-      const double work = (rounds > f.alone ? rounds : f.alone) / s, way = memory * (m < 160 ? 1.6 : m < 256 ? 256 / m : 1);  // (what few workgroups draw)
+      const double work = (rounds > f.alone ? rounds : f.alone) / s, way = memory * (m < 160 ? 1.6 : m < 256 ? 256 / m : m > 512 && s > 1 ? 1.15 : 1);  // (few workgroups draw less; a second round costs a start)
       const double ends = a->kv_len ? 1 + 0.25 / s : 1;  // (of ragged sequences the last pieces are half empty)
       const double merge = s == 1 ? 0 : fused ? 1500 + 100.0 * s * (packed < 8 ? packed : 8) / 8
                                               : 6000 + 60.0 * s + (double)per_split * (s * 8 / 3000. + 0.4 / a->dh);
