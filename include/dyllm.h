@@ -447,7 +447,8 @@ int dyllm_page_plan(dyllm_ctx *ctx, const dyllm_pages *pages, int32_t R, const i
  *   axis_pos[axis[p]][j] * rope_theta^(-2p/dh),  axis_pos: [n_axes, rows->cap], axis: HOST array [dh/2] of values below n_axes,
  * positions of either sign and any size.  n_axes <= 8.  axis_pos NULL: every pair takes rows->pos[j] (n_axes and axis are not looked at).
  * q_out[j], [count, H, dh]; keys and values go to rows->slot[j].  A slot of -1 (or below) drops them; one behind the last page drops them too
- * and sets the status word to DYLLM_ERR_INVALID_ARG.  pages->table is not looked at.  rows->cap may exceed the context's max_rows. */
+ * and sets the status word to DYLLM_ERR_INVALID_ARG.  Rows of a call have different slots (a place that two rows go to holds pieces of either).
+ * pages->table is not looked at.  rows->cap may exceed the context's max_rows. */
 int dyllm_head_norm_rope_paged(dyllm_ctx *ctx, const void *qkv, int64_t ld, const void *g_q, const void *g_k,
                                const dyllm_page_rows *rows, int32_t R, const int32_t *axis_pos, int32_t n_axes,
                                const uint8_t *host_axis, const dyllm_pages *pages, void *q_out, void *stream);
@@ -461,7 +462,7 @@ int dyllm_head_norm_rope_paged(dyllm_ctx *ctx, const void *qkv, int64_t ld, cons
  *                neighbours, keys of other documents cost no time.
  * A row that no key counts for is zero.  Keys that do not count have no influence, infinities and NaN among them. */
 typedef struct {
-  float cap;             /* 0: none */
+  float cap;             /* 0: none; else from 2^-20 to 4096 (a score is off by up to 2^-20 of it) */
   int32_t block;         /* 0: all keys count */
   const int32_t *prefix; /* NULL or [B] (R) */
   const float *slopes;   /* NULL or [H] */

@@ -681,6 +681,8 @@ int check_page_rows(dyllm_ctx *ctx, const dyllm_page_rows *r, bool pos, bool slo
 int check_scores(dyllm_ctx *ctx, const dyllm_scores *s, bool pages) {
   if (!s) return DYLLM_OK;
   if (!(s->cap >= 0.f) || isinf(s->cap)) return fail(ctx, DYLLM_ERR_INVALID_ARG, "scores: cap is negative or no finite number");
+  // (x is q.k scaled in fp32: a cap below 2^-20 of it is a sign, above 4096 the difference of two numbers of the cap's size loses it)
+  if (s->cap > 0.f && (s->cap < 0x1p-20f || s->cap > 4096.f)) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "scores: cap is not from 2^-20 to 4096");
   if (s->block < 0) return fail(ctx, DYLLM_ERR_INVALID_ARG, "scores: negative block");
   if (pages && s->doc) return fail(ctx, DYLLM_ERR_UNSUPPORTED, "scores: documents over pages");
   if (((uintptr_t)s->prefix | (uintptr_t)s->slopes | (uintptr_t)s->doc) & 3) return fail(ctx, DYLLM_ERR_INVALID_ARG, "scores: misaligned");

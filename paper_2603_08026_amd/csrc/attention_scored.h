@@ -90,7 +90,7 @@ struct ScoredItem {
   int counter = 0;  // number of the (tile, key-value head)
 };
 struct ScoredSeq { int lo = 0, rows = 0, tiles = 0, keys = 0; };
-__device__ __forceinline__ int scored_rows(const ScoredAttn &a) { return a.offsets ? min(a.offsets[a.B], a.cap) : a.B * a.L; }
+__device__ __forceinline__ int scored_rows(const ScoredAttn &a) { return a.offsets ? max(min(a.offsets[a.B], a.cap), 0) : a.B * a.L; }
 __device__ __forceinline__ ScoredSeq scored_seq(const ScoredAttn &a, int b, int total) {
   ScoredSeq q;
   if (b >= a.B) return q;
@@ -399,7 +399,8 @@ __device__ __forceinline__ void doc_range(const int32_t *doc, int n, int lo, int
 // A row's part in the masks and the scores' shape.
 struct RowMask {
   int limit = 0, doc = -1;
-  float pos = 0.f, slope = 0.f;  // slope in units of the score as it goes into the exponential's multiply-add
+  int pos = 0;        // (distances are taken between whole numbers: positions may exceed 2^24)
+  float slope = 0.f;  // slope in units of the score as it goes into the exponential's multiply-add
 };
 
 // x = q.k (not scaled) -> reshaped; x * sc is in log2 units (a capped one is so itself: sc = 1)
@@ -498,7 +499,7 @@ __device__ __forceinline__ bool shape_scores(floatx16 &s, const Shape &sh, const
   }
   if constexpr (MODE & BIASED) {
     if (MODE != DOCS_ANY || sh.sloped) {
-      const float d0 = row.pos - (float)key0;
+      const float d0 = (float)(row.pos - key0);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = fmaf(-row.slope, fabsf(d0 - (float)(8 * (e / 4) + (e % 4))), s[e]);
     }

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_f32(ScoredAttn a) {
   for (int r = 0; r < R; ++r) {  // (rows past the end: the last one again, their results are never stored)
     const int rr = min(r, nq - 1), i = position_of(a, PAGED, b, row_of(rr));
     row[r].limit = limit_of(a, b, item.keys, i);
-    row[r].pos = (float)i;
+    row[r].pos = i;
     row[r].slope = a.slopes ? a.slopes[head_of(rr)] * LOG2E : 0.f;  // (scores are kept in the log2 domain)
     if (docs) {
       row[r].doc = i >= 0 && i < a.L ? docs[i] : -1;
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_f32(ScoredAttn a) {
       }
       float x = lanes_sum<LPK>(d0 + d1);
       if (sh.capped) x = sh.cap_out * tanhf(x);
-      if (sh.sloped) x = fmaf(-row[r].slope, fabsf(row[r].pos - (float)key), x);
+      if (sh.sloped) x = fmaf(-row[r].slope, fabsf((float)(row[r].pos - key)), x);
       if (tested) x = key < k_hi && key < row[r].limit && (!docs || now.doc == row[r].doc) ? x : -INFINITY;
       score[r] = x;
       need = need || x > m_run[r] + 8.0f;
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(LIST_NT) void k_scored_list(ScoredAttn a) {
 template <int DH>
 __global__ __launch_bounds__(256) void k_scored_merge(ScoredAttn a) {
   constexpr int V = DH / WAVE;
-  const int n = a.offsets ? min(a.offsets[a.B], a.cap) : a.cap, lane = threadIdx.x % WAVE;
+  const int n = scored_rows(a), lane = threadIdx.x % WAVE;
   const uint32_t items = (uint32_t)n * (uint32_t)a.H;
   const size_t step = (size_t)a.cap * a.H;
   for (uint32_t it = blockIdx.x * 4 + threadIdx.x / WAVE; it < items; it += gridDim.x * 4) {

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
   {
     const int i = position_of(a, PAGED, b, jq);
     row.limit = limit_of(a, b, item.keys, i);
-    row.pos = (float)i;
+    row.pos = i;
     if ((MODE & BIASED) && a.slopes) row.slope = sh.slope(a.slopes[hq]);
     if constexpr (MODE & DOCS) {
       row.doc = i >= 0 && i < a.L ? a.doc[(size_t)b * a.L + i] : -1;
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
   {
     const int i = position_of(a, PAGED, b, jq);
     row.limit = limit_of(a, b, item.keys, i);
-    row.pos = (float)i;
+    row.pos = i;
     if ((MODE & BIASED) && a.slopes) row.slope = sh.slope(a.slopes[hq]);
     int lo = 0x7fffffff, hi = -1;
     if constexpr (MODE & DOCS) {
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_many(ScoredAttn a) {
       for (int kk = 0; kk < KK / 2; ++kk) read_k(kk);
       // Reshaping and the test of limits: behind the first products, without a branch; other tests ahead of everything.
       const int k0 = k_lo + t * TK, below = row.limit - (k0 + 4 * lhi);
-      const float d0 = row.pos - (float)(k0 + 4 * lhi);
+      const float d0 = (float)(row.pos - (k0 + 4 * lhi));
       bool tested = TEST == LIMIT;
       if constexpr (TEST == ALL)
         tested = shape_scores<MODE>(s_cur, sh, row, tests, k0, lhi, l32, reinterpret_cast<const int32_t *>(st + 2 * T::REGION + wave * 256));

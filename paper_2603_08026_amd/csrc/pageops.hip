@@ -205,7 +205,7 @@ template <typename T, int DH>
 __global__ __launch_bounds__(PH_NT) void k_heads_paged(PagedHeads a, int per, int parts) {
   constexpr int LPH = DH / 16, HPW = WAVE / LPH, HALF = DH / 2;
   __shared__ float2 table[PH_WAVES][HALF];
-  const int n = min(*a.rows.count, a.rows.cap);
+  const int n = max(min(*a.rows.count, a.rows.cap), 0);
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, sub = lane % LPH;
   const int HT = a.H + 2 * a.Hkv, P = 1 << a.pages.shift;
   const long slots = (long)a.pages.n_pages << a.pages.shift;

@@ -106,6 +106,9 @@ int main(int argc, char **argv) {
   say("cap -1", score([&](auto &s) { s.cap = -1.f; }));
   say("cap -1", score([&](auto &s) { s.cap = INFINITY; }));
   say("cap -1", score([&](auto &s) { s.cap = NAN; }));
+  say("cap -3", score([&](auto &s) { s.cap = 1e-7f; }));
+  say("cap -3", score([&](auto &s) { s.cap = 4097.f; }));
+  say("cap 0", score([&](auto &s) { s.cap = 4096.f; }));
   say("block -1", score([&](auto &s) { s.block = -1; }));
   say("odd slopes -1", score([&](auto &s) { s.slopes = (const float *)odd(x); }));
   say("documents -3", score([&](auto &s) { s.doc = len; }));

@@ -386,6 +386,44 @@ def test_attention_of_a_chunk_beside_single_tokens(t, H, Hkv, dh, lengths, count
     check_paged(25, t, H, Hkv, dh, 16, list(lengths), list(counts), "causal")
 
 
+@pytest.mark.parametrize("t,H,rows", [("bf16", 2, 1), ("bf16", 64, 3), ("f32", 2, 2)])
+def test_positions_beyond_24_bits(t, H, rows):
+    """A request of 2^24 + 5001 tokens, whose pages are few and used over and over: distances between positions that fp32 does not hold."""
+    say("paged attention, positions beyond 24 bits", t, H, rows)
+    g = W.philox(27, t)
+    dh, P, n, held = 64, 1024, 2 ** 24 + 5001, 7
+    ctx = context(t, H, 1, dh)
+    k, v = (dev(g.standard_normal((held, 1, P, dh)), t) for _ in range(2))
+    width = -(-n // P)
+    pages = Bd.Pages(k, v, ints((np.arange(width) % held)[None]))
+    slopes = np.where(np.arange(H) % 2 == 0, 0.5, 0.25)
+    pos = np.arange(n - rows, n)
+    q = dev(g.standard_normal((rows, H, dh)), t)
+    out = torch.zeros(rows, H * dh, dtype=TD[t], device="cuda")
+    ctx.paged_attention(q, pages, Bd.PageRows(ints([0, rows]), ints(pos), ints(np.zeros(rows))), ints([n]), out, Bd.Scores(block=1, slopes=dev(slopes)))
+    torch.cuda.synchronize()
+    near = np.arange(n - 1500, n)  # (a key further away weighs less than e^(12 - 375) of the nearest ones)
+    kk, vv = (host(x)[near // P % held, 0, near % P][:, None] for x in (k, v))
+    want, tol = attend(host(q), kk, vv, pos - near[0], t, slopes=slopes, block=1)
+    within(out, want, tol, "rows")
+    ctx.close()
+
+
+def test_counts_below_zero():
+    """Offsets that no plan leaves: no row is read or written."""
+    say("paged attention and heads, a negative count")
+    ctx = context("bf16", 2, 1, 64)
+    pages = Bd.Pages.empty(4, 1, 16, 64, 2, 2, torch.bfloat16)
+    before = pages.k.clone()
+    rows = Bd.PageRows(ints([0, 3, -5]), ints([0, 1, 2]), ints([0, 1, 2]))
+    q, out = torch.ones(3, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.full((3, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx.head_norm_rope_paged(torch.ones(3, 256, dtype=torch.bfloat16, device="cuda"), None, None, rows, pages, q)
+    ctx.paged_attention(q, pages, rows, ints([16, 16]), out)
+    torch.cuda.synchronize()
+    assert torch.all(q == 1.0) and torch.all(out == 7.0) and torch.equal(pages.k, before)
+    ctx.close()
+
+
 @pytest.mark.parametrize("R", [64, 65, 128, 129, 1100])
 @pytest.mark.parametrize("t,H,Hkv,dh", [("bf16", 4, 1, 64), ("bf16", 2, 2, 128), ("f32", 2, 1, 64)])
 def test_attention_of_more_requests_than_lanes(t, H, Hkv, dh, R):
