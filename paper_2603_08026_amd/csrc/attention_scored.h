@@ -304,7 +304,7 @@ __device__ __forceinline__ const unsigned char *uniform_bytes(const void *p) {
 }
 // Where the keys and values of a sequence and head lie.  A tile of 32 keys starts at a multiple of 32, pages hold a multiple of 16: its two halves
 // lie each in one piece.  PAGED: their pages are asked for through the scalar cache, a tile ahead.
-template <bool PAGED, int DH> struct KeyPlaces {
+template <bool PAGED, int DH, int BYTES = 2> struct KeyPlaces {  // BYTES of an element
   const unsigned char *k, *v;             // of key 0 (pages: of page 0)
   uint32_t stride;                        // bytes from one key to the next
   const __attribute__((address_space(4))) int32_t *table;
@@ -313,19 +313,19 @@ template <bool PAGED, int DH> struct KeyPlaces {
   int ahead[2];                           // pages of the tile asked for
   __device__ __forceinline__ KeyPlaces(const ScoredAttn &a, int b, int kvh) {
     if constexpr (PAGED) {
-      const size_t head = ((size_t)kvh << a.pages.shift) * DH * 2;
+      const size_t head = ((size_t)kvh << a.pages.shift) * DH * BYTES;
       k = uniform_bytes((const unsigned char *)a.pages.k + head);
       v = uniform_bytes((const unsigned char *)a.pages.v + head);
-      stride = DH * 2;
+      stride = DH * BYTES;
       table = (const __attribute__((address_space(4))) int32_t *)uniform_bytes(a.pages.table + (size_t)b * a.pages.max_pages);
-      page_bytes = ((size_t)a.Hkv << a.pages.shift) * DH * 2;
+      page_bytes = ((size_t)a.Hkv << a.pages.shift) * DH * BYTES;
       shift = a.pages.shift;
       n_pages = a.pages.n_pages;
     } else {
-      const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH * 2;
+      const size_t first = ((size_t)b * a.L * a.Hkv + kvh) * DH * BYTES;
       k = uniform_bytes((const unsigned char *)a.k + first);
       v = uniform_bytes((const unsigned char *)a.v + first);
-      stride = (uint32_t)a.Hkv * DH * 2;
+      stride = (uint32_t)a.Hkv * DH * BYTES;
     }
   }
   __device__ __forceinline__ void ask(int k0, int last) {  // (entries behind the last key are not looked at)

@@ -59,7 +59,7 @@ def test_turns(probe, theta, dh):
 @pytest.mark.parametrize("t,H,Hkv,dh,pages,B,L,rows,bq,split", [
     (1, 32, 32, 128, 1, 1, 4096, 1, 128, True), (1, 28, 4, 128, 1, 32, 32768, 32, 128, True), (1, 32, 32, 128, 1, 16, 1280, 512, 128, False),
     (1, 28, 4, 128, 1, 4, 8192, 8192, 128, False), (1, 32, 32, 128, 0, 16, 1280, 2048, 128, False), (1, 8, 2, 64, 0, 2, 200, 2, 32, False),
-    (0, 4, 4, 64, 1, 1, 4096, 1, 2, True), (0, 4, 4, 64, 0, 2, 1000, 800, 2, False)])
+    (0, 4, 4, 64, 1, 1, 4096, 1, 2, True), (0, 4, 4, 64, 0, 2, 1000, 800, 32, False)])
 def test_plans(probe, t, H, Hkv, dh, pages, B, L, rows, bq, split):
     """Few rows of long sequences split their keys, many do not, and no plan has more splits than its scratch or 128."""
     got = [int(x) for x in probe("plan", t, H, Hkv, dh, pages, B, L, rows)[0].split(" ")]
