@@ -10,7 +10,8 @@ namespace {
 
 // ---- 32 packed rows a workgroup: few rows ----------------------------------------------------------------------
 // Bound by the keys' and values' way from memory.  The four waves share nothing: each streams key tiles of its own (tile wave, wave + 4, ..) through
-// its own ring in LDS, with no barrier in the loop; their results are merged once at the end.
+// its own ring in LDS, with no barrier in the loop; their results are merged once at the end.  8 rows of each of 4 sequences of 512 keys, 32 heads of 128, 15 us
+// where the tile of 128 takes 17; of long sequences the deeper ring of that tile draws more (one token of 32 requests of 11000 to 32768 keys: all choices there).
 template <int DH, int MODE> struct FewTile : KeyTile<DH> {
   using K = KeyTile<DH>;
   static constexpr int NW = 4, NS = DH == 128 ? 2 : 4, BQ = 32;
@@ -235,7 +236,9 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
 // Four waves of 32 rows over shared tiles of 32 keys, four stages in LDS, two workgroups a CU; the loop is that of k_attn_bf16_dma: while the
 // vector ALU takes the exponentials of tile t, the matrix pipe works through P V of tile t - 1 and the scores of tile t + 1, and the copies of tile
 // t + 3 go out one behind each few products.  Tiles that need no test run in a loop unrolled over the stages; a tile that may need one, and the last
-// ones, in a body with the tests.
+// ones, in a body with the tests.  Bound by the exponentials beside the matrix pipe: 4096 rows of 4096 keys without masks 1090 to 1140 TFLOP/s, what the
+// library's product of 8192 x 8192 matrices reaches; 4 chunks of 2048 rows in causal order over up to 8192 keys 514 us, 967 TFLOP/s of what counts (the
+// tiles on the diagonal are whole).  Few rows: by the way from memory, one token of 32 requests of 11000 to 32768 keys, 28 heads over 4, 236 us, 6.3 TB/s.
 template <int DH, int MODE> struct ManyTile : KeyTile<DH> {
   using K = KeyTile<DH>;
   static constexpr int NW = 4, NS = 4, BQ = 128;
