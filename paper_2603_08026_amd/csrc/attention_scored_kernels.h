@@ -10,8 +10,8 @@ namespace {
 
 // ---- 32 packed rows a workgroup: few rows ----------------------------------------------------------------------
 // Bound by the keys' and values' way from memory.  The four waves share nothing: each streams key tiles of its own (tile wave, wave + 4, ..) through
-// its own ring in LDS, with no barrier in the loop; their results are merged once at the end.  8 rows of each of 4 sequences of 512 keys, 32 heads of 128, 15 us
-// where the tile of 128 takes 17; of long sequences the deeper ring of that tile draws more (one token of 32 requests of 11000 to 32768 keys: all choices there).
+// its own ring in LDS, with no barrier in the loop; their results are merged once at the end.  8 rows of each of 4 sequences of 512 keys, 32 heads of 128, 14.0 us
+// where the tile of 128 takes 16.6; from long sequences that tile's copies past the L2, two workgroups a CU, draw more.
 template <int DH, int MODE> struct FewTile : KeyTile<DH> {
   using K = KeyTile<DH>;
   static constexpr int NW = 4, NS = DH == 128 ? 2 : 4, BQ = 32;

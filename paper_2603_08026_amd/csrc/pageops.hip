@@ -17,7 +17,7 @@ namespace {
 // position lies in.  So the sums are made once a workgroup, in LDS, and rows, taken pages and pages that go back to the list are dealt out
 // by their numbers, each finding its request by a binary search: no workgroup waits for another, long prompts are shared out, and the
 // result does not depend on the order of anything.
-// Bound by the launch and the chain load - scan - search - load - store: 64 decoded tokens 2.7 us, 1500 requests with chunks of up to 512 tokens 8.3.
+// Bound by the launch and the chain load - scan - search - load - store: 64 decoded tokens 2.7 us, 1500 requests with chunks of up to 512 tokens 8.8.
 constexpr int MANY = 1 << 30;  // sums stop here
 __device__ __forceinline__ int sat(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)MANY); }
 template <int CTRL, int ROWS> __device__ __forceinline__ int sat_step(int x) {
