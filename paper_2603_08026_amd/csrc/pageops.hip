@@ -108,7 +108,8 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
     }
   }
   __syncthreads();
-  const int released = carry[2], n_free = min(max(free_word, 0), pages.n_pages), have = sat(n_free, released);
+  // (below MANY, so that a sum of gains that has stopped there is more than there are)
+  const int released = carry[2], n_free = min(max(free_word, 0), pages.n_pages), have = min(sat(n_free, released), MANY - 1);
   // pages taken: the gains of the served requests, which are a prefix of those that gain
   int taken = carry[1];
   if (taken > have) {
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
     return pages.table[(size_t)r * pages.max_pages + request(r).need + (k - before_of(loss_to, r))];
   };
   auto taken_page = [&](int k) { return k < released ? released_page(k) : a.free_list[n_free - 1 - (k - released)]; };
-  auto served = [&](int r) { return gain_to[r] <= have || gain_to[r] == before_of(gain_to, r); };
+  auto served = [&](int r, const Req &q) { return q.fits && (q.need <= q.held || gain_to[r] <= have); };  // (two sums say nothing where both have stopped)
   // rows, table entries gained, pages that go back, requests: one after the other in number
   const int total = sat(sat(n_rows, taken), sat(left, R));
   for (int i = blockIdx.x * NT + tid; i < total; i += gridDim.x * NT) {
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
       const int p = q.start + (k - before_of(rows_to, r)), e = p >> shift;
       a.pos[k] = p;
       int slot = -1;
-      if (q.fits && served(r)) {
+      if (served(r, q)) {
         const int page = e < q.held ? pages.table[(size_t)r * pages.max_pages + e] : taken_page(before_of(gain_to, r) + (e - q.held));
         slot = (int)(((uint32_t)page << shift) | (uint32_t)(p & ((1 << shift) - 1)));
       }
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
     }
     k -= taken;
     if (k < left) {
-      const int at = n_free + k;
+      const int at = sat(n_free, k);
       if (at < pages.n_pages) a.free_list[at] = released_page(taken + k);
       continue;
     }
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
       a.n_free_out[0] = min(have - taken, pages.n_pages);
     }
     const Full f = read(k);
-    a.len_out[k] = f.q.fits && served(k) ? f.then : f.len;
+    a.len_out[k] = served(k, f.q) ? f.then : f.len;
     a.offsets[k + 1] = min(rows_to[k], a.cap);
   }
 }

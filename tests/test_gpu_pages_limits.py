@@ -1,0 +1,43 @@
+"""The page accounting where sums of pages pass 2^30."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_08026_amd import binding as Bd
+from tests.test_gpu_pages import context, ints, say
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("greedy,width", [(16, 2 ** 26), (2048, 2 ** 19)])
+def test_gains_beyond_30_bits(greedy, width):
+    """Requests that ask for 2^30 pages together, then one that asks for one page, one that gives a page back, one that stays: none behind the first that
+    does not fit gains anything, and all others go on."""
+    say("page plan: gains of 2^30 pages", greedy, width)
+    P, n_pages = 16, 9
+    R = 1 + greedy + 3
+    ctx = context("bf16", 4, 2, 64, 16)
+    k = torch.zeros(n_pages, 1, P, 8, dtype=torch.bfloat16, device="cuda")
+    table = torch.full((R, width), -77, dtype=torch.int32, device="cuda")
+    table[0, 0], table[R - 2, 0], table[R - 2, 1], table[R - 1, 0] = 4, 5, 6, 7
+    length, new, rows = np.zeros(R, int), np.full(R, width * P), np.ones(R, int)
+    length[[0, R - 2, R - 1]] = 10, 20, 9
+    new[[0, R - 3, R - 2, R - 1]] = 20, 16, 16, 9
+    out = Bd.PageRows(*(ints(np.full(n, -99)) for n in (R + 1, R, R)))
+    free, len_out, n_out = ints([0, 1, 2] + [-88] * 6), ints(np.full(R, -99)), ints([-99])
+    pages = Bd.Pages(k, k.clone(), table)
+    for _ in range(2):  # (a repeated call leaves the same)
+        ctx.page_plan(pages, ints(length), ints(new), ints(rows), free, ints([3]), out, len_out, n_out)
+        assert ctx.poll_status() == Bd.ERR_CAPACITY
+        # request 0 takes the lost page 6; the pool is as before
+        want = length.copy()
+        want[[0, R - 2]] = 20, 16
+        assert np.array_equal(len_out.cpu(), want) and int(n_out) == 3
+        assert np.array_equal(free.cpu(), [0, 1, 2] + [-88] * 6)
+        slot = np.full(R, -1)
+        slot[[0, R - 2, R - 1]] = 6 * P + 3, 5 * P + 15, 7 * P + 8
+        assert np.array_equal(out.slot.cpu(), slot)
+        assert np.array_equal(out.pos.cpu(), new - 1) and np.array_equal(out.offsets.cpu(), np.arange(R + 1))
+        assert table[0, :3].tolist() == [4, 6, -77] and table[R - 2, :3].tolist() == [5, 6, -77] and table[R - 1, :2].tolist() == [7, -77]
+        assert not torch.any(table[1:R - 2] != -77)
+    ctx.close()
