@@ -126,11 +126,11 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
   };
   auto taken_page = [&](int k) { return k < released ? released_page(k) : a.free_list[n_free - 1 - (k - released)]; };
   auto served = [&](int r, const Req &q) { return q.fits && (q.need <= q.held || gain_to[r] <= have); };  // (two sums say nothing where both have stopped)
-  // rows, table entries gained, pages that go back, requests: one after the other in number
-  const int total = sat(sat(n_rows, taken), sat(left, R));
-  for (int i = blockIdx.x * NT + tid; i < total; i += gridDim.x * NT) {
-    int k = i;
-    if (k < n_rows) {
+  // rows, table entries gained, pages that go back, requests: one after the other in number (each at most MANY: 32 bits hold their sum)
+  const uint32_t total = (uint32_t)n_rows + (uint32_t)taken + (uint32_t)left + (uint32_t)R;
+  for (uint32_t i = blockIdx.x * NT + tid; i < total; i += gridDim.x * NT) {
+    if (i < (uint32_t)n_rows) {
+      const int k = (int)i;
       const int r = first_above(rows_to, R, k);
       const Req q = request(r);
       const int p = q.start + (k - before_of(rows_to, r)), e = p >> shift;
@@ -143,19 +143,20 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
       a.slot[k] = slot;
       continue;
     }
-    k -= n_rows;
-    if (k < taken) {
+    uint32_t rest = i - (uint32_t)n_rows;
+    if (rest < (uint32_t)taken) {
+      const int k = (int)rest;
       const int r = first_above(gain_to, R, k);
       pages.table[(size_t)r * pages.max_pages + request(r).held + (k - before_of(gain_to, r))] = taken_page(k);
       continue;
     }
-    k -= taken;
-    if (k < left) {
-      const int at = sat(n_free, k);
+    rest -= (uint32_t)taken;
+    if (rest < (uint32_t)left) {
+      const int k = (int)rest, at = sat(n_free, k);
       if (at < pages.n_pages) a.free_list[at] = released_page(taken + k);
       continue;
     }
-    k -= left;
+    const int k = (int)(rest - (uint32_t)left);
     if (k == 0) {
       a.offsets[0] = 0;
       a.n_free_out[0] = min(have - taken, pages.n_pages);

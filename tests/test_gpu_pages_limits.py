@@ -1,4 +1,4 @@
-"""The page accounting where sums of pages pass 2^30."""
+"""The page accounting where sums of pages and of rows pass 2^30."""
 import numpy as np
 import pytest
 import torch
@@ -40,4 +40,48 @@ def test_gains_beyond_30_bits(greedy, width):
         assert np.array_equal(out.pos.cpu(), new - 1) and np.array_equal(out.offsets.cpu(), np.arange(R + 1))
         assert table[0, :3].tolist() == [4, 6, -77] and table[R - 2, :3].tolist() == [5, 6, -77] and table[R - 1, :2].tolist() == [7, -77]
         assert not torch.any(table[1:R - 2] != -77)
+    ctx.close()
+
+
+def test_lengths_of_more_pages_than_there_are():
+    """Lengths that claim 2^30 pages, more than a pool can have: what is given back in excess is dropped, and nothing outside the lists is touched."""
+    say("page plan: losses of 2^30 pages")
+    P, n_pages, width, R = 16, 6, 2 ** 26, 18
+    ctx = context("bf16", 4, 2, 64, 16)
+    k = torch.zeros(n_pages, 1, P, 8, dtype=torch.bfloat16, device="cuda")
+    table = torch.full((R, width), 3, dtype=torch.int32, device="cuda")
+    length, new = np.full(R, width * P), np.zeros(R, int)
+    length[R - 1], new[R - 1] = 0, 16
+    out = Bd.PageRows(*(ints(np.full(n, -99)) for n in (R + 1, R, R)))
+    guard = ints(np.full(n_pages + 64, -88))
+    len_out, n_out = ints(np.full(R, -99)), ints([-99])
+    ctx.page_plan(Bd.Pages(k, k.clone(), table), ints(length), ints(new), ints(new > 0), guard[:n_pages], ints([0]), out, len_out, n_out)
+    torch.cuda.synchronize()
+    assert np.array_equal(len_out.cpu(), new) and int(n_out) == n_pages
+    assert np.array_equal(guard.cpu(), [3] * n_pages + [-88] * 64) and int(out.slot[0]) == 3 * P + 15
+    ctx.poll_status()
+    ctx.close()
+
+
+def test_rows_beyond_30_bits():
+    """As many rows as a capacity may have, beside the pages that they take: every output is there."""
+    say("page plan: 2^30 rows")
+    P, each, R = 1024, 2 ** 29, 3
+    cap, n_pages, width = 2 * each, 2 * each // P + 1, each // P
+    ctx = context("bf16", 4, 2, 64, 16)
+    none = torch.zeros(n_pages, 1, P, 0, dtype=torch.bfloat16, device="cuda")  # (the plan looks at no key)
+    pages = Bd.Pages(none, none, torch.full((R, width), -77, dtype=torch.int32, device="cuda"))
+    rows = Bd.PageRows(ints([-99] * (R + 1)), *(torch.full((cap,), -99, dtype=torch.int32, device="cuda") for _ in range(2)))
+    len_out, n_out = ints([-99] * R), ints([-99])
+    free = torch.arange(n_pages, dtype=torch.int32, device="cuda")
+    ctx.page_plan(pages, ints([0] * R), ints([each, each, 1]), ints([each, each, 0]), free, ints([n_pages]), rows, len_out, n_out)
+    assert ctx.poll_status() == 0
+    assert len_out.tolist() == [each, each, 1] and int(n_out) == 0 and rows.offsets.tolist() == [0, each, cap, cap]
+    taken = n_pages - 1 - torch.arange(2 * width, dtype=torch.int32, device="cuda")  # from the top of the stack
+    assert torch.equal(pages.table[:2].view(-1), taken) and int(pages.table[2, 0]) == 0
+    step = 2 ** 26
+    for at in range(0, cap, step):
+        i = torch.arange(at, at + step, dtype=torch.int32, device="cuda")
+        assert torch.equal(rows.pos[at:at + step], i % each)
+        assert torch.equal(rows.slot[at:at + step], taken[(i // P).long()] * P + i % P)
     ctx.close()
