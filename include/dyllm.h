@@ -472,14 +472,15 @@ typedef struct {
 /* Attention of the rows over the keys and values of their requests' pages: row j is the query at position rows->pos[j].
  * q: [count, H, dh]; out: [count, H*dh]; kv_len: [R] tokens of each request whose keys are in place, the new ones among them (clamped to what
  * the table can hold).  scores: NULL for plain attention in both directions.  rows->slot is not looked at (may be NULL).  Table entries that name
- * no page of the pool are read as its first page, and set the status word to DYLLM_ERR_INVALID_ARG.  R <= DYLLM_MAX_REQUESTS; R and
+ * no page of the pool are read as its first page, and set the status word to DYLLM_ERR_INVALID_ARG.  Offsets that descend set it too, and nothing is written
+ * into out.  R <= DYLLM_MAX_REQUESTS; R and
  * rows->cap may exceed the context's max_batch and max_rows (which the scratch for key splits goes by).  Roundings as in dyllm_partial_attention_quant; kernel and key splits are chosen by rows->cap, R and
  * max_pages on the host and by the lengths on the device. */
 int dyllm_paged_attention(dyllm_ctx *ctx, const void *q, const dyllm_pages *pages, const dyllm_page_rows *rows, int32_t R,
                           const int32_t *kv_len, const dyllm_scores *scores, void *out, void *stream);
 
 /* dyllm_partial_attention with masked and reshaped scores.  kv_len: NULL, or [B] keys of each sequence (clamped to [0, L]); rows == NULL means
- * all B*L tokens.  q_sal: [count, H, dh]; k_cache, v_cache: [B, L, Hkv, dh]; c_sal_out: [count, H*dh]. */
+ * all B*L tokens.  q_sal: [count, H, dh]; k_cache, v_cache: [B, L, Hkv, dh]; c_sal_out: [count, H*dh].  Offsets that descend: as over pages. */
 int dyllm_partial_attention_masked(dyllm_ctx *ctx, const void *q_sal, const void *k_cache, const void *v_cache,
                                    const int32_t *kv_len, const dyllm_index_list *rows, int32_t B, int32_t L,
                                    const dyllm_scores *scores, void *c_sal_out, void *stream);

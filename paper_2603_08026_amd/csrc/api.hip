@@ -698,7 +698,7 @@ ScoredAttn scored_args(const dyllm_ctx *ctx, const void *q, const dyllm_scores *
   a.part_o = ctx->part_o; a.part_ml = ctx->part_ml; a.part_elems = ctx->quant_part_elems;
   a.arrive = ctx->arrive; a.list = ctx->list;
   a.n_split = (int32_t *)ctx->cosb; a.split_rows = ctx->rows_cap;
-  a.status = ctx->status; a.bad_page_code = DYLLM_ERR_INVALID_ARG;
+  a.status = ctx->status; a.bad_page_code = a.bad_offsets_code = DYLLM_ERR_INVALID_ARG;
   return a;
 }
 

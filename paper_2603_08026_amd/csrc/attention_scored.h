@@ -150,18 +150,28 @@ __device__ __forceinline__ void scored_fill(const ScoredAttn &a, ScoredItem &it,
   it.splits = split_count(q.keys, it.chunk);
   it.split = mine / q.tiles;
   const int tile = q.tiles - 1 - mine % q.tiles;  // the last rows of a causal sequence have the most keys: they come first
-  it.counter = min(it.kv_head * n_tiles + tiles_before + tile, ARRIVE_WORDS - 1);  // (more tiles than the host counted: offsets that do not ascend)
+  it.counter = it.kv_head * n_tiles + tiles_before + tile;  // (below ARRIVE_WORDS where there are splits: scored_plan)
   it.packed = tile * a.bq;
   it.n = min(a.bq, q.rows * (a.H / a.Hkv) - it.packed);
 }
+// Offsets that descend name some rows twice: that would be more tiles than the grid and the counters were made for, and a counter that never comes to its
+// end stays for later calls.  So a call with such offsets has no items at all, and says so in the status word.
+__device__ __forceinline__ bool descends(const ScoredAttn &a, int b) { return a.offsets && b < a.B && a.offsets[b + 1] < a.offsets[b]; }
 // Up to 64 sequences: every workgroup looks at all of them, a lane at one.  More: k_scored_list has left, for every sequence, the items and tiles of it and
 // those before it, and the size of the pieces; a search over 64 equal parts, then inside one.
-constexpr int LIST_HEAD = 1;  // words before the two lists: the size of the pieces
+constexpr int LIST_HEAD = 1;  // words before the two lists: the size of the pieces, 0 where offsets descend
+__device__ __forceinline__ bool no_order(const ScoredAttn &a) {  // uniform
+  return a.B <= WAVE ? __any(descends(a, threadIdx.x % WAVE)) : a.list[0] == 0;
+}
 __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
   const int lane = threadIdx.x % WAVE, total = scored_rows(a);
   ScoredItem it;
   int w;
   if (a.B <= WAVE) {
+    if (no_order(a)) {
+      if (p == 0 && threadIdx.x == 0) *a.status = a.bad_offsets_code;
+      return it;
+    }
     const ScoredSeq q = scored_seq(a, lane, total);
     const int chunk = scored_chunk(a, [&](auto f) { return wave_fold(f(q), Sum{}); });
     const int upto = wave_scan(q.tiles * split_count(q.keys, split_size(a, q.keys, chunk))), tiles_to = wave_scan(q.tiles);

@@ -460,6 +460,13 @@ __global__ __launch_bounds__(LIST_NT) void k_scored_list(ScoredAttn a) {
   __shared__ int ends[2][LIST_NW];
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
   const int total = scored_rows(a), per = (a.B + LIST_NT - 1) / LIST_NT, first = tid * per;
+  bool down = false;
+  for (int i = 0; i < per; ++i) down = down || descends(a, first + i);
+  if (__syncthreads_or(down)) {  // no items
+    for (int i = tid; i <= 2 * a.B; i += LIST_NT) a.list[i] = 0;
+    if (tid == 0) *a.status = a.bad_offsets_code;
+    return;
+  }
   const int chunk = scored_chunk(a, [&](auto f) {
     float x = 0.f;
     for (int i = 0; i < per; ++i) x += f(scored_seq(a, first + i, total));  // (a sequence that is not there has no tiles)
@@ -504,10 +511,11 @@ __global__ __launch_bounds__(LIST_NT) void k_scored_list(ScoredAttn a) {
 template <int DH>
 __global__ __launch_bounds__(256) void k_scored_merge(ScoredAttn a) {
   constexpr int V = DH / WAVE;
+  if (no_order(a)) return;
   const int n = scored_rows(a), lane = threadIdx.x % WAVE;
-  const uint32_t items = (uint32_t)n * (uint32_t)a.H;
+  const uint32_t items = (uint32_t)n * (uint32_t)a.H, first = a.offsets ? (uint32_t)max(a.offsets[0], 0) * (uint32_t)a.H : 0u;  // (rows ahead are no sequence's)
   const size_t step = (size_t)a.cap * a.H;
-  for (uint32_t it = blockIdx.x * 4 + threadIdx.x / WAVE; it < items; it += gridDim.x * 4) {
+  for (uint32_t it = first + blockIdx.x * 4 + threadIdx.x / WAVE; it < items; it += gridDim.x * 4) {
     const int splits = min(a.n_split[it / (uint32_t)a.H], a.splits);
     if (splits <= 1) continue;  // (the row is finished)
     float m[2], l[2];

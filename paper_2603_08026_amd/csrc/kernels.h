@@ -253,7 +253,7 @@ struct ScoredAttn {
   int32_t *n_split = nullptr;      // splits of every row, for as many rows as split_rows; nullptr: the splits are not merged by a launch of their own
   int split_rows = 0;
   int32_t *status = nullptr;
-  int bad_page_code = 0;
+  int bad_page_code = 0, bad_offsets_code = 0;
   // chosen by scored_plan: rows of a tile, most splits of a sequence, workgroups to split for, whether the last one merges, copies past the L2
   int bq = 0, splits = 1, target = 0;
   bool fused = false, once = false;
