@@ -250,7 +250,19 @@ def _int32s(what: str, *tensors):
     return [t.data_ptr() for t in tensors]
 
 
-class Pages:
+class _Held:
+    """What is made of tensors once, `c` with their addresses last: another tensor would change nothing in calls, and its forerunner could be freed."""
+
+    def __setattr__(self, name, value):
+        if "c" in self.__dict__:
+            raise AttributeError("%s.%s stays as it was made: make another" % (type(self).__name__, name))
+        self.__dict__[name] = value
+
+    def __delattr__(self, name):
+        raise AttributeError("%s.%s stays as it was made" % (type(self).__name__, name))
+
+
+class Pages(_Held):
     """Pages of keys and values: k, v [n_pages, Hkv, page_size, dh] and the page table, int32 [R, max_pages]."""
 
     def __init__(self, k, v, table):
@@ -270,7 +282,7 @@ class Pages:
         return Pages(k, v, torch.zeros(R, max_pages, dtype=torch.int32, device=device))
 
 
-class PageRows:
+class PageRows(_Held):
     """The rows of a call over pages: int32 offsets [R+1], pos and slot [cap]."""
 
     def __init__(self, offsets, pos, slot):
@@ -286,7 +298,7 @@ class PageRows:
         return PageRows(*(torch.zeros(n, dtype=torch.int32, device=device) for n in (R + 1, cap, cap)))
 
 
-class Scores:
+class Scores(_Held):
     """What becomes of attention scores (dyllm_scores).  prefix: int32 [B]; slopes: fp32 [H]; doc: int32 [B, L]; device tensors or None."""
 
     def __init__(self, cap: float = 0.0, block: int = 0, prefix=None, slopes=None, doc=None):
