@@ -462,7 +462,7 @@ int dyllm_head_norm_rope_paged(dyllm_ctx *ctx, const void *qkv, int64_t ld, cons
  *                neighbours, keys of other documents cost no time.
  * A row that no key counts for is zero.  Keys that do not count have no influence, infinities and NaN among them. */
 typedef struct {
-  float cap;             /* 0: none; else from 2^-20 to 4096 (a score is off by up to 2^-20 of it) */
+  float cap;             /* 0: none; else from 2^-20 to 4096 (bf16: a score is off by up to 2^-20 of it) */
   int32_t block;         /* 0: all keys count */
   const int32_t *prefix; /* NULL or [B] (R) */
   const float *slopes;   /* NULL or [H] */

@@ -432,6 +432,14 @@ struct Shape {
   }
 };
 
+// fp32: tanh by itself, as exact for small scores as for large ones (the difference of two numbers of the cap's size loses what a score is smaller: 4.9e-4 of
+// a score of 1 at a cap of 4096).  200 rows of each of 16 sequences of 2048 keys, 16 heads over 4 of 128: no cap 598 us, a cap 682, by the difference 623.
+struct ShapeF32 : Shape {
+  float cap_by;  // 1 / (sqrt(dh) cap)
+  __device__ __forceinline__ ShapeF32(const ScoredAttn &a) : Shape(a) { cap_by = capped ? 1.0f / sqrtf((float)a.dh) / a.soft_cap : 0.f; }
+  __device__ __forceinline__ float cap(float x) const { return cap_out * tanhf(x * cap_by); }
+};
+
 // Values that are no finite numbers, in a tile where some keys count for some rows only.  A matrix product gives 0 * inf = NaN to rows that the key does
 // not count for.  So these values are taken out, and what they do to rows with a weight for them is found by products with 0 and 1 (is it NaN,
 // +inf, -inf) in place of the values.  Rare: no cost beyond the look at the values of tiles that are tested key by key.
@@ -498,8 +506,8 @@ struct TileTests {
 };
 // Scores of a lane's 16 keys of the tile at k0, reshaped; keys that do not count -> -inf.  Returns whether any was tested (uniform).  docs: the tile's
 // 32 numbers in LDS.
-template <int MODE>
-__device__ __forceinline__ bool shape_scores(floatx16 &s, const Shape &sh, const RowMask &row, const TileTests &t, int k0, int lhi, int l32, const int32_t *docs) {
+template <int MODE, typename SHAPE>
+__device__ __forceinline__ bool shape_scores(floatx16 &s, const SHAPE &sh, const RowMask &row, const TileTests &t, int k0, int lhi, int l32, const int32_t *docs) {
   const int key0 = k0 + 4 * lhi;
   if constexpr (MODE & CAPPED) {
     if (MODE != DOCS_ANY || sh.capped) {

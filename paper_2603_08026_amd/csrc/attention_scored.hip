@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void k_scored_f32_tile(Score
   // this lane's query (rows past the end: the last one again, their results are never stored)
   const int p = item.packed + min(l32, nq - 1), jq = item.row + p / grp, hq = kvh * grp + p % grp;
   const uint32_t place = (uint32_t)jq * (uint32_t)a.H + (uint32_t)hq;
-  const Shape sh(a);
+  const ShapeF32 sh(a);
   RowMask row;
   TileTests tests;
   int k_lo = split * item.chunk;

@@ -22,3 +22,6 @@ SPLITS = [
     dense("bf16", 4, 4, 128, 3, 2000, 36, 128, "launch"), dense("bf16", 8, 2, 128, 70, 1000, 210, 128, "launch", True, lengths=True),
     dense("bf16", 4, 2, 64, 70, 1000, 210, 128, "last", True), paged("bf16", 4, 2, 64, 3, 3008, 12, 32, "last"), paged("f32", 4, 2, 64, 3, 3008, 12, 2, "last"),
 ]
+
+# Caps in fp32 (test_gpu_scored_caps.py)
+CAPS = [dense("f32", 8, 2, 64, 1, 200, 3, 2), dense("f32", 4, 4, 128, 1, 200, 5, 2, "last"), dense("f32", 8, 2, 64, 1, 500, 500, 32), dense("f32", 8, 8, 128, 1, 500, 400, 32)]

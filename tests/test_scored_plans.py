@@ -38,5 +38,6 @@ def held(s, plan):
 
 def test_shapes_of_the_gpu_tests(plans):
     """Every call of the tests on the GPU gets the kernel that it is there for."""
-    for s, plan in zip(S.SPLITS, plans(S.SPLITS)):
+    shapes = S.SPLITS + S.CAPS
+    for s, plan in zip(shapes, plans(shapes)):
         held(s, plan)
