@@ -11,6 +11,8 @@
 //   workgroups that pieces are made for, elements of the scratch for partial rows, rows that the merge's launch has room for, counters
 int main() {
   int v[13];
+  dyllm_layer_cfg made{};
+  dyllm_ctx *ctx = nullptr;
   for (;;) {
     for (int &x : v)
       if (scanf("%d", &x) != 1) return 0;
@@ -18,8 +20,12 @@ int main() {
     cfg.hidden = 256; cfg.ffn_dim = 256; cfg.rms_eps = 1e-5f; cfg.rope_theta = 1e4f;
     cfg.dtype = v[0] ? DYLLM_BF16 : DYLLM_F32; cfg.n_heads = v[1]; cfg.n_kv_heads = v[2]; cfg.head_dim = v[3];
     cfg.max_batch = v[10]; cfg.max_seq = v[11]; cfg.max_rows = v[12];
-    dyllm_ctx *ctx = nullptr;
-    if (dyllm_create(&cfg, &ctx) != DYLLM_OK) return 3;
+    if (!ctx || memcmp(&cfg, &made, sizeof(cfg))) {  // (the one of the line before, where that is the same)
+      if (ctx) dyllm_destroy(ctx);
+      ctx = nullptr;
+      if (dyllm_create(&cfg, &ctx) != DYLLM_OK) return 3;
+      made = cfg;
+    }
     ScoredAttn a = scored_args(ctx, nullptr, nullptr, nullptr);
     int32_t some = 0;
     a.pages.table = v[4] ? &some : nullptr;
@@ -30,6 +36,5 @@ int main() {
     const long g = a.H / a.Hkv, tiles = a.offsets ? (a.cap * g + a.bq - 1) / a.bq + a.B : a.B * ((a.L * g + a.bq - 1) / a.bq);
     printf("%d %d %d %d %d %ld %d %zu %d %d\n", a.bq, a.splits, a.fused, a.once, a.n_split != nullptr, tiles * a.Hkv, a.target, a.part_elems, a.split_rows,
            ARRIVE_WORDS);
-    dyllm_destroy(ctx);
   }
 }

@@ -40,3 +40,31 @@ def test_shapes_of_the_gpu_tests(plans):
     """Every call of the tests on the GPU gets the kernel that it is there for."""
     for s, plan in zip(S.ALL, plans(S.ALL)):
         held(s, plan)
+
+
+def test_plans_fit_their_scratch(plans):
+    """Partial rows fit the context's scratch, splits the merge's lanes, tiles of split keys the counters, rows the words of a launch's merge: also for lists
+    of more rows than the context was made for."""
+    shapes = []
+    for t in ("bf16", "f32"):
+        for H, Hkv, dh in ((2, 1, 64), (8, 2, 64), (28, 4, 128), (32, 32, 128), (64, 1, 128)):
+            for pages, room in ((True, 1), (True, 64), (True, 4096), (False, 0)):
+                for B in (1, 3, 64, 65, 300):
+                    for L in (16, 1600, 40000):
+                        if not pages and (L > 1600 or B * L * H * dh > 2 ** 27):
+                            continue
+                        for cap in sorted({1, B, 8 * B, 9 * B, 100 * B, 5000}):
+                            if pages or cap <= B * L:
+                                shapes.append(S.Shape(t, H, Hkv, dh, pages, True, pages or B % 2 == 1, B, L, cap, room or L, 0, False, "", False))
+    kinds = set()
+    for s, plan in zip(shapes, plans(shapes)):
+        bq, splits, fused, once, launch, tiles, target, elems, rows, counters = plan
+        assert 1 <= splits <= 128, (s, plan)
+        if splits > 1:
+            assert splits * s.cap * s.H * s.dh <= elems, (s, plan)
+            assert 0 < target <= 1024, (s, plan)
+            assert bool(launch) != bool(fused), (s, plan)
+            assert not fused or tiles <= counters, (s, plan)
+            assert not launch or s.cap <= rows, (s, plan)
+        kinds.add((s.t, bq, "" if splits == 1 else "launch" if launch else "last"))
+    assert kinds == {("f32", 2, ""), ("f32", 2, "last"), ("f32", 32, ""), ("f32", 32, "last"), *(("bf16", n, m) for n in (32, 128) for m in ("", "last", "launch"))}
