@@ -168,14 +168,14 @@ __device__ __forceinline__ ScoredItem scored_item(const ScoredAttn &a, int p) {
   ScoredItem it;
   int w;
   if (a.B <= WAVE) {
-    if (no_order(a)) {
-      if (p == 0 && threadIdx.x == 0) *a.status = a.bad_offsets_code;
-      return it;
-    }
     const ScoredSeq q = scored_seq(a, lane, total);
+    const bool down = no_order(a);
     const int chunk = scored_chunk(a, [&](auto f) { return wave_fold(f(q), Sum{}); });
     const int upto = wave_scan(q.tiles * split_count(q.keys, split_size(a, q.keys, chunk))), tiles_to = wave_scan(q.tiles);
-    if (!scored_place(a, p, __builtin_amdgcn_readlane(upto, WAVE - 1), &it.kv_head, &w)) return it;
+    if (!scored_place(a, p, down ? 0 : __builtin_amdgcn_readlane(upto, WAVE - 1), &it.kv_head, &w)) {
+      if (down) *a.status = a.bad_offsets_code;  // (all threads: with one picked out the documents' kernel spills 26 registers in place of 9, 269 -> 277 us)
+      return it;
+    }
     const int f = __ffsll((unsigned long long)__ballot(upto > w)) - 1;
     const int before = f ? __builtin_amdgcn_readlane(upto, f - 1) : 0, tiles_before = f ? __builtin_amdgcn_readlane(tiles_to, f - 1) : 0;
     auto of = [&](int x) { return __builtin_amdgcn_readlane(x, f); };
