@@ -649,7 +649,7 @@ class Context:
             shape = axis_pos.shape
             if len(shape) != 2 or shape[1] != n or axis is None or len(axis) != self._dh // 2:
                 raise ValueError("axis_pos: [n_axes, %d] and an axis for each of %d pairs are wanted" % (n, self._dh // 2))
-            n_axes, axis = shape[0], axis if type(axis) is bytes else bytes(iter(axis))  # (number by number: arrays hand out their memory)
+            n_axes, axis = shape[0], bytes(axis if type(axis) in (bytes, list, tuple) else iter(axis))  # (number by number: arrays hand out their memory)
             axis_pos = self._arg(axis_pos, n_axes * n, "axis_pos", dev, torch.int32)
         else:
             axis = None
