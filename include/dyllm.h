@@ -460,7 +460,8 @@ int dyllm_head_norm_rope_paged(dyllm_ctx *ctx, const void *qkv, int64_t ld, cons
  *                j < prefix[b] (prefixes see themselves and are seen by all)
  *   doc:         the key counts only if doc of both tokens is the same and not negative (padding).  Any numbers in any order; where equal ones are
  *                neighbours, keys of other documents cost no time.
- * A row that no key counts for is zero.  Keys that do not count have no influence, infinities and NaN among them. */
+ * A row that no key counts for is zero.  Keys that do not count have no influence, infinities and NaN among them.  A key whose score is -infinity weighs
+ * nothing; a row all of whose keys do is zero too. */
 typedef struct {
   float cap;             /* 0: none; else from 2^-20 to 4096 (bf16: a score is off by up to 2^-20 of it) */
   int32_t block;         /* 0: all keys count */

@@ -46,4 +46,7 @@ TILE_PAGES = [paged("f32", 8, 2, 64, 4, 384, 460, 32), paged("f32", 8, 8, 128, 4
 # Values that are no numbers, in both
 NO_NUMBER = [dense("bf16", 16, 16, 128, 1, 1000, 700, 128, room=4096), dense("bf16", 32, 4, 64, 1, 1000, 800, 128, room=4096),
              dense("f32", 8, 8, 128, 1, 200, 150, 32, room=4096), dense("f32", 8, 8, 64, 1, 200, 150, 32, room=4096)]
-ALL = (SPLITS + CAPS + MANY + MANY_LENGTHS + MANY_ALL + MANY_SPLIT + MANY_PAGES + TILE + TILE_LENGTHS + TILE_ALL + TILE_SPLIT + TILE_PAGES + NO_NUMBER)
+# Scores without a bound, in each of the four kernels (test_gpu_scored_infinite.py)
+INFINITE = [dense("bf16", 4, 2, 64, 1, 200, 20, 32, room=4096), dense("bf16", 16, 16, 128, 1, 1000, 700, 128, room=4096), dense("f32", 8, 2, 64, 1, 200, 3, 2),
+            dense("f32", 8, 8, 128, 1, 200, 150, 32, room=4096)]
+ALL = (SPLITS + CAPS + MANY + MANY_LENGTHS + MANY_ALL + MANY_SPLIT + MANY_PAGES + TILE + TILE_LENGTHS + TILE_ALL + TILE_SPLIT + TILE_PAGES + NO_NUMBER + INFINITE)

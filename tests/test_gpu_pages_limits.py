@@ -1,10 +1,11 @@
-"""The page accounting where sums of pages and of rows pass 2^30."""
+"""Requests over pages, and attention with shaped scores, where sums of pages and rows pass 2^30 and tensors 2^32 bytes."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2603_08026_amd import binding as Bd
-from tests.test_gpu_pages import context, ints, say
+from synth import workload as W
+from tests.test_gpu_pages import TD, attend, context, dev, heads, heads_tol, host, ints, say, within
 
 pytestmark = pytest.mark.gpu
 
@@ -84,4 +85,61 @@ def test_rows_beyond_30_bits():
         i = torch.arange(at, at + step, dtype=torch.int32, device="cuda")
         assert torch.equal(rows.pos[at:at + step], i % each)
         assert torch.equal(rows.slot[at:at + step], taken[(i // P).long()] * P + i % P)
+    ctx.close()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("counts", [(1, 1), (300, 150)])
+def test_pools_beyond_4_gib(t, counts):
+    """Rows into pages, and attention over them, of a pool whose tensors have more than 2^32 bytes each."""
+    say("a pool beyond 4 GiB", t, counts)
+    H, Hkv, dh, P, lengths = 8, 2, 128, 64, (300, 150)
+    n_pages = 2 ** 32 // (Hkv * P * dh * TD[t].itemsize) + 40
+    g, ctx = W.philox(15, t), context(t, H, Hkv, dh, 512)
+    k, v = (torch.empty(n_pages, Hkv, P, dh, dtype=TD[t], device="cuda") for _ in range(2))
+    table = np.concatenate([n_pages - 1 - g.permutation(7), [3, n_pages // 2 + 1, 0]])[:10].reshape(2, 5)
+    pages = Bd.Pages(k, v, ints(table))
+    pos = np.concatenate([np.arange(n) for n in lengths])
+    slot = np.concatenate([table[r, np.arange(n) // P] * P + np.arange(n) % P for r, n in enumerate(lengths)])
+    qkv = dev(g.standard_normal((450, (H + 2 * Hkv) * dh)), t)
+    q = torch.zeros(450, H, dh, dtype=TD[t], device="cuda")
+    ctx.head_norm_rope_paged(qkv, None, None, Bd.PageRows(ints([0, 300, 450]), ints(pos), ints(slot)), pages, q)
+    x = host(qkv).reshape(450, H + 2 * Hkv, dh)
+    y, size = heads(x[:, H:H + Hkv], None, pos[None].astype(float), np.zeros(dh // 2, int))
+    page, place = torch.from_numpy(slot // P).cuda(), torch.from_numpy(slot % P).cuda()
+    within(k[page, :, place], y, heads_tol(y, size, t), "k")
+    assert np.array_equal(host(v[page, :, place]), x[:, H + Hkv:])
+    take = np.concatenate([np.arange(300 - counts[0], 300), np.arange(450 - counts[1], 450)])
+    rows = Bd.PageRows(ints([0, counts[0], sum(counts)]), ints(pos[take]), ints(slot[take]))
+    qs, out = q[torch.from_numpy(take).cuda()], torch.zeros(len(take), H * dh, dtype=TD[t], device="cuda")
+    ctx.paged_attention(qs, pages, rows, ints(lengths), out, Bd.Scores(block=1))
+    stored = host(k[page, :, place])
+    for r, (lo, n) in enumerate(((0, 300), (300, 150))):
+        rr = slice(0, counts[0]) if r == 0 else slice(counts[0], None)
+        want, tol = attend(host(qs)[rr], stored[lo:lo + n], x[lo:lo + n, H + Hkv:], pos[take][rr], t, block=1)
+        within(out[rr], want, tol, "request %d" % r)
+    assert ctx.poll_status() == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [3, 300])
+def test_sequences_beyond_4_gib(t, m):
+    """A sequence of [B, L] caches whose keys lie more than 2^32 bytes apart: rows at its end, in a document of the last tokens."""
+    say("a sequence beyond 4 GiB", t, m)
+    H, Hkv, dh = 32, 32, 64
+    L = 2 ** 32 // (Hkv * dh * TD[t].itemsize) + 777
+    g = W.philox(16, t)
+    ctx = Bd.Context(Bd.LayerCfg(256, H, Hkv, dh, 256, 1, L, 512, Bd.F32 if t == "f32" else Bd.BF16, 1e-5, 1e4))
+    k, v = (torch.zeros(1, L, Hkv, dh, dtype=TD[t], device="cuda") for _ in range(2))
+    last = 500
+    for x in (k, v):
+        x[0, L - last:] = dev(g.standard_normal((last, Hkv, dh)), t)
+    doc = torch.zeros(1, L, dtype=torch.int32, device="cuda")
+    doc[0, L - last + 40:] = 9
+    idx = np.arange(L - m, L)
+    q, out = dev(g.standard_normal((m, H, dh)), t), torch.zeros(m, H * dh, dtype=TD[t], device="cuda")
+    ctx.partial_attention_masked(q, k, v, Bd.IndexList(ints(idx), ints([0, m])), 1, L, out, Bd.Scores(block=1, doc=doc))
+    want, tol = attend(host(q), host(k[0, L - last + 40:]), host(v[0, L - last + 40:]), idx - (L - last + 40), t, block=1)
+    within(out, want, tol, "rows")
     ctx.close()
