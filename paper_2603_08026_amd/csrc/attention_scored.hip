@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void k_scored_f32(ScoredAttn a) {
 // its own; V of a tile is on its way during the scores, K of the next one during the product with V.
 // Bound by the matrix pipe (2 x 2 dh x 32 x 32 operations a tile at 256 a cycle and CU) and the loads' addresses, a line a lane for K.  200 rows of each of
 // 16 requests of 2048 keys, 16 heads over 4 of 128: 597 us, 90 TFLOP/s (two rows a workgroup: 2955); 8 heads over 2 of 64 176 / 797; 32 rows of each
-// of 4 of 512, 4 heads of 64, 17.4 / 13.5.
+// of 4 of 512, 4 heads of 64, 17.4 / 13.5.  (71 to 143 scalar registers go to lanes of vector registers, none to memory.)
 template <int DH, bool PAGED>
 __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void k_scored_f32_tile(ScoredAttn a) {
   constexpr int TK = 32, DB = DH / 32, HALF = DH / 2, NW = 4, PER_WAVE = (DB * 16 + 2) * 64;

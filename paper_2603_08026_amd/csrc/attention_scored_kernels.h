@@ -237,8 +237,9 @@ __global__ __launch_bounds__(256, 1) void k_scored_few(ScoredAttn a) {
 // vector ALU takes the exponentials of tile t, the matrix pipe works through P V of tile t - 1 and the scores of tile t + 1, and the copies of tile
 // t + 3 go out one behind each few products.  Tiles that need no test run in a loop unrolled over the stages; a tile that may need one, and the last
 // ones, in a body with the tests.  Bound by the exponentials beside the matrix pipe: 4096 rows of 4096 keys without masks 1090 to 1140 TFLOP/s, what the
-// library's product of 8192 x 8192 matrices reaches; 4 chunks of 2048 rows in causal order over up to 8192 keys 514 us, 967 TFLOP/s of what counts (the
+// library's product of 8192 x 8192 matrices reaches; 4 chunks of 2048 rows in causal order over up to 8192 keys 514 to 530 us, 940 to 967 TFLOP/s of what counts (the
 // tiles on the diagonal are whole).  Few rows: by the way from memory, one token of 32 requests of 11000 to 32768 keys, 28 heads over 4, 236 us, 6.3 TB/s.
+// (Documents with heads of 128 spill 9 vector registers, all outside the loops.)
 template <int DH, int MODE> struct ManyTile : KeyTile<DH> {
   using K = KeyTile<DH>;
   static constexpr int NW = 4, NS = 4, BQ = 128;

@@ -17,7 +17,8 @@ namespace {
 // position lies in.  So the sums are made once a workgroup, in LDS, and rows, taken pages and pages that go back to the list are dealt out
 // by their numbers, each finding its request by a binary search: no workgroup waits for another, long prompts are shared out, and the
 // result does not depend on the order of anything.
-// Bound by the launch and the chain load - scan - search - load - store: 64 decoded tokens 2.7 us, 1500 requests with chunks of up to 512 tokens 8.8.
+// Bound by the launch and the chain load - scan - search - load - store: 64 decoded tokens 2.7 us, 1500 requests with chunks of up to 512 tokens 9.4
+// (medians of a kernel trace).
 constexpr int MANY = 1 << 30;  // sums stop here
 __device__ __forceinline__ int sat(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)MANY); }
 template <int CTRL, int ROWS> __device__ __forceinline__ int sat_step(int x) {
@@ -171,7 +172,8 @@ __global__ __launch_bounds__(NT) void k_page_plan(Pages pages, PagePlan a) {
 // As k_heads (headops.hip) takes a head: dh / 16 lanes, 8 neighbouring columns of each half a lane.  Here a wave takes `per` groups of
 // heads of one row, and with them the row's angles once: a lane computes cosine and sine of one pair and leaves them in LDS.
 //   angle = pos * f turns, f = theta^(-2p/dh) / 2 pi, held in 2^-64 turns: the product modulo 2^64 is the angle's fraction of a turn with whole
-// turns gone, exact to 2^-33 turns at any 32-bit position.  Its nearest quarter turn leaves |x| <= pi / 4, where the series of sine and
+// turns gone, right to 2^-31 turns at any 32-bit position (the factor's rounding times the position, and the low word that
+// is cut off: 2^-32 each).  Its nearest quarter turn leaves |x| <= pi / 4, where the series of sine and
 // cosine end with x^9 and x^10 (what is left out is below 2e-9 and 2e-10).
 // Bound by the rows' way in and out: 8192 rows of 32 + 2 x 32 heads of 128 in bf16, 403 MB, 76 us (5.3 TB/s); of few rows by the launch (3 us).
 __device__ __forceinline__ float2 cos_sin(uint64_t f, int pos) {
