@@ -475,7 +475,8 @@ typedef struct {
  * the table can hold).  scores: NULL for plain attention in both directions.  rows->slot is not looked at (may be NULL).  Table entries that name
  * no page of the pool are read as its first page, and set the status word to DYLLM_ERR_INVALID_ARG.  Offsets that descend set it too, and nothing is written
  * into out.  R <= DYLLM_MAX_REQUESTS; R and
- * rows->cap may exceed the context's max_batch and max_rows (which the scratch for key splits goes by).  Roundings as in dyllm_partial_attention_quant; kernel and key splits are chosen by rows->cap, R and
+ * rows->cap may exceed the context's max_batch and max_rows.  (The scratch for key splits goes by max_rows, and what of it a call may use by rows->cap: where lists have more room than
+ * max_rows, few rows of long requests are split less or not at all.)  Roundings as in dyllm_partial_attention_quant; kernel and key splits are chosen by rows->cap, R and
  * max_pages on the host and by the lengths on the device. */
 int dyllm_paged_attention(dyllm_ctx *ctx, const void *q, const dyllm_pages *pages, const dyllm_page_rows *rows, int32_t R,
                           const int32_t *kv_len, const dyllm_scores *scores, void *out, void *stream);
